@@ -7,12 +7,17 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
+CSRC_ITER = os.path.join(HERE, "csrc_iter")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libgnr_sim.so")
 OBJ = os.path.join(HERE, "_build")
 # every policy variant of the step kernel is a translation unit of its own, so that they compile side by side
 STEP_VARIANTS = ["plain", "rr", "im", "ab", "ab_rr", "ab_im", "ws"]
 SOURCES = ["gnr_kernels.hip", "gnr_api.cpp", "gnr_tables.cpp"] + [f"gnr_step_{v}.hip" for v in STEP_VARIANTS]
+# the operators of a batch iteration
+ITER_SOURCES = ["gnr_iter_api.cpp", "gnr_iter_cache.hip", "gnr_iter_attention.hip", "gnr_iter_adapters.hip"]
+ITER_HEADERS = [os.path.join(CSRC_ITER, "gnr_iter_internal.h"), os.path.join(CSRC_ITER, "gnr_iter_device.h"),
+                os.path.join(INCLUDE, "gnr_iter.h"), os.path.join(INCLUDE, "gnr_sim.h")]
 HEADERS = [os.path.join(CSRC, "gnr_step.h"), os.path.join(CSRC, "gnr_internal.h"), os.path.join(INCLUDE, "gnr_sim.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=off",
@@ -32,15 +37,19 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=o
          # servers x 2048 replications (17.9 -> 18.5 ms per 1000 steps) and with the convergence instance, 4 % with the weighted
          # router (9.0 -> 9.3 per 300), 1 % with 2048 x 1024, nothing with 10000 x 256, and give 1 % with 256 x 1024
          "-mllvm", "-disable-lsr", "-mllvm", "-disable-machine-licm"]
+# the rest of the flags are about the step kernel's registers and atomics
+ITER_FLAGS = FLAGS[:FLAGS.index("-Wno-unused-function") + 1]
 
 
 def _compile(src: str, force: bool, verbose: bool) -> str:
-    path = os.path.join(CSRC, src)
+    iteration = src in ITER_SOURCES
+    csrc = CSRC_ITER if iteration else CSRC
+    path = os.path.join(csrc, src)
     obj = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-    deps = [path] + HEADERS
+    deps = [path] + (ITER_HEADERS if iteration else HEADERS)
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) > os.path.getmtime(d) for d in deps):
         return obj
-    cmd = [HIPCC] + FLAGS + [f"-I{INCLUDE}", f"-I{CSRC}", "-c", path, "-o", obj]
+    cmd = [HIPCC] + (ITER_FLAGS if iteration else FLAGS) + [f"-I{INCLUDE}", f"-I{csrc}", "-c", path, "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -55,9 +64,10 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
 def build(verbose: bool = False, force: bool = True, jobs: int | None = None) -> str:
     """Compiles every source (all of them when `force`, else those older than their object) and links the library."""
     os.makedirs(OBJ, exist_ok=True)
-    jobs = jobs or min(len(SOURCES), os.cpu_count() or 1, 16)
+    sources = SOURCES + ITER_SOURCES
+    jobs = jobs or min(len(sources), os.cpu_count() or 1, 16)
     with ThreadPoolExecutor(jobs) as pool:
-        objs = list(pool.map(lambda s: _compile(s, force, verbose), SOURCES))
+        objs = list(pool.map(lambda s: _compile(s, force, verbose), sources))
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + objs + ["-o", LIB]
     if verbose:
         print(" ".join(cmd), flush=True)

@@ -1,0 +1,61 @@
+// Element types and small device functions of the iteration operators (gfx950).
+#ifndef GNR_ITER_DEVICE_H
+#define GNR_ITER_DEVICE_H
+
+#include <hip/hip_runtime.h>
+
+#include "gnr_iter_internal.h"
+
+namespace gnr {
+
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) short s16x2;
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+
+template <class To, class From>
+__device__ __forceinline__ To bits(From f)
+{
+  static_assert(sizeof(To) == sizeof(From), "same size");
+  return __builtin_bit_cast(To, f);
+}
+
+// The 16-bit types: T::from_e4m3 reads two codes (the lower or upper half of a word) times a power of two, exactly but for
+// what leaves the type's range; T::to_e4m3 is its inverse, rounded to nearest even, for values within 448 * 2^e.
+struct Bf16 {
+  typedef __bf16 elem;
+  typedef bf16x2 pair;
+  typedef bf16x8 oct;
+  static constexpr uint32_t kInf = 0x7F80u;
+  static __device__ __forceinline__ float widen(uint32_t w) { return bits<float>(w << 16); }
+  static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<__bf16>(a), static_cast<__bf16>(b)}; return bits<uint32_t>(p); }
+  template <bool kUpper>
+  static __device__ __forceinline__ uint32_t from_e4m3(uint32_t codes, float scale) { return bits<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, kUpper)); }
+  template <bool kUpper>
+  static __device__ __forceinline__ s16x2 to_e4m3(s16x2 codes, uint32_t w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(codes, bits<pair>(w), scale, kUpper); }
+};
+struct Fp16 {
+  typedef _Float16 elem;
+  typedef f16x2 pair;
+  typedef f16x8 oct;
+  static constexpr uint32_t kInf = 0x7C00u;
+  static __device__ __forceinline__ float widen(uint32_t w) { return static_cast<float>(bits<_Float16>(static_cast<uint16_t>(w))); }
+  static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<_Float16>(a), static_cast<_Float16>(b)}; return bits<uint32_t>(p); }
+  template <bool kUpper>
+  static __device__ __forceinline__ uint32_t from_e4m3(uint32_t codes, float scale) { return bits<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, kUpper)); }
+  template <bool kUpper>
+  static __device__ __forceinline__ s16x2 to_e4m3(s16x2 codes, uint32_t w, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(codes, bits<pair>(w), scale, kUpper); }
+};
+
+__device__ __forceinline__ float exponent_scale(uint32_t byte) { return bits<float>(byte << 23); }
+
+inline int iter_hip_ok(hipError_t e) { return e == hipSuccess ? SIM_OK : SIM_EHIP; }
+
+}  // namespace gnr
+#endif

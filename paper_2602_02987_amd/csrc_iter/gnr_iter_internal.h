@@ -1,0 +1,46 @@
+// Shared by the host side and the kernels of the operators of one batch iteration.
+#ifndef GNR_ITER_INTERNAL_H
+#define GNR_ITER_INTERNAL_H
+
+#include <cstddef>
+#include <cstdint>
+
+#include "gnr_iter.h"
+
+namespace gnr {
+
+struct AttentionParams {
+  iter_cache cache;
+  iter_batch batch;
+  iter_rows q, out;
+  int type, heads, group;      // group: query heads to a kv head
+  int page_shift;
+  float scale_log2;            // scale / ln 2: weights are powers of two
+  int64_t window;
+  float *workspace;
+  size_t bytes;
+  uint32_t *status;
+};
+
+struct AdapterParams {
+  iter_adapter_set set;
+  int type, requests;
+  int64_t tokens;
+  const int32_t *q_start, *adapter;
+  const void *x, *base;
+  void *out;
+  int64_t x_stride, base_stride, out_stride;
+  float *workspace;
+  uint32_t *status;
+};
+
+// All return a sim_err; arguments have been checked.
+int launch_kv_write(const iter_cache &c, int type, const iter_rows &k, const iter_rows &v, const int64_t *slots, int64_t tokens, void *stream);
+int launch_kv_read(const iter_cache &c, int type, const iter_rows &k, const iter_rows &v, const int64_t *slots, int64_t tokens, void *stream);
+size_t attention_bytes(const iter_cache &c, const iter_batch &b, int heads);
+int launch_attention(const AttentionParams &p, void *stream);
+size_t adapters_bytes(const iter_adapter_set &s, int64_t tokens);
+int launch_adapters(const AdapterParams &p, void *stream);
+
+}  // namespace gnr
+#endif

@@ -1,0 +1,584 @@
+"""The iteration operators on the GPU against plain 64-bit implementations (tests/iteration_reference.py), at the sizes, layouts
+and contents where they can go wrong."""
+import numpy as np
+import pytest
+import torch
+
+import iteration_reference as R
+from paper_2602_02987_amd import iteration as I
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+def _gen(seed):
+    g = torch.Generator()
+    g.manual_seed(seed)
+    return g
+
+
+def _filled_cache(gen, pages, heads, places, dim, kind, token_major=False):
+    """A cache with random contents, exponents that differ from row to row."""
+    shape = (pages, heads, places, dim)
+    x = torch.randn(shape, generator=gen)
+    ke = ve = None
+    if kind == "fp8":
+        k, v = ((torch.randn(shape, generator=gen) * 100).clamp(-448, 448).to(torch.float8_e4m3fn) for _ in range(2))
+        ke, ve = (torch.randint(115, 122, shape[:3], generator=gen, dtype=torch.uint8) for _ in range(2))
+    else:
+        k, v = x.to(R.TYPES[kind]), torch.randn(shape, generator=gen).to(R.TYPES[kind])
+
+    def laid(t):
+        if t is None:
+            return None
+        t = t.to(DEV)
+        if not token_major:
+            return t
+        b = t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t
+        b = b.transpose(1, 2).contiguous().transpose(1, 2)
+        return b.view(t.dtype) if t.dtype == torch.float8_e4m3fn else b
+    return tuple(laid(t) for t in (k, v, ke, ve))
+
+
+def _batch(gen, q_len, kv_len, pages, places, width=None):
+    need = [-(-n // places) for n in kv_len]
+    order = torch.randperm(pages, generator=gen).to(torch.int32)
+    width = width or max(need + [1])
+    table = torch.full((len(q_len), width), 0, dtype=torch.int32)
+    at = 0
+    for r, n in enumerate(need):
+        table[r, :n] = order[at:at + n]
+        at += n
+    assert at <= pages
+    start = torch.tensor(np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32))
+    return table, start, torch.tensor(kv_len, dtype=torch.int32)
+
+
+# (heads, kv_heads, dim, page, q type, cache, new tokens, cached tokens, window, token-major)
+ATTENTION = [
+    (4, 2, 128, 16, "bf16", "bf16", [1], [1], 0, False),                                          # one token, one key
+    (8, 2, 128, 16, "bf16", "bf16", [1, 1, 1], [5, 64, 65], 0, False),
+    (8, 2, 64, 16, "fp16", "fp16", [1, 1, 1, 1], [31, 32, 33, 700], 0, True),
+    (8, 1, 256, 32, "bf16", "bf16", [1, 1], [300, 257], 0, False),                                # one kv head for all
+    (7, 1, 128, 64, "bf16", "fp8", [1, 1, 1], [127, 128, 1000], 0, False),                        # seven heads to a kv head
+    (6, 2, 64, 16, "fp16", "fp8", [1, 1], [63, 2000], 0, True),
+    (2, 2, 256, 16, "fp16", "fp8", [1, 2, 3], [40, 2, 513], 0, False),
+    (4, 4, 128, 1, "bf16", "bf16", [1, 1], [37, 80], 0, False),                                   # pages of one token
+    (4, 2, 128, 1024, "bf16", "bf16", [1, 3], [130, 700], 0, False),                              # a page larger than the request
+    (32, 1, 64, 16, "bf16", "bf16", [1, 1], [100, 257], 0, False),                                # more heads than a tile of rows
+    (48, 2, 128, 16, "bf16", "fp8", [1, 2, 1], [90, 300, 1], 0, False),
+    (8, 2, 128, 16, "bf16", "bf16", [33], [33], 0, False),                                        # a prompt from an empty cache
+    (8, 2, 128, 64, "fp16", "fp16", [130], [700], 0, False),                                      # a chunk after others
+    (4, 1, 64, 16, "bf16", "bf16", [257], [257], 0, True),
+    (14, 2, 128, 16, "fp16", "fp8", [61], [333], 0, False),
+    (3, 1, 256, 32, "bf16", "fp8", [100], [201], 0, False),
+    (2, 1, 256, 16, "fp16", "fp16", [129], [129], 0, False),
+    (8, 2, 128, 16, "bf16", "bf16", [1, 40, 0, 1, 70, 1], [90, 40, 11, 1, 200, 400], 0, False),    # chunks among decodes, one without a token
+    (16, 4, 64, 32, "bf16", "fp8", [1, 1, 65, 1], [200, 1, 300, 77], 0, False),
+    (8, 2, 128, 16, "bf16", "bf16", [1, 1, 50, 200], [300, 5, 300, 200], 17, False),               # a window
+    (8, 2, 64, 16, "fp16", "fp8", [1, 1, 130], [300, 64, 400], 1, False),                         # every token sees itself alone
+    (4, 2, 128, 16, "bf16", "bf16", [1, 3, 40, 1], [0, 1, 10, 20], 0, False),                      # tokens before the first key: rows without any
+    (4, 2, 128, 16, "bf16", "fp8", [1, 5, 70, 1], [0, 0, 0, 3], 9, False),
+    (28, 4, 128, 16, "fp16", "fp8", [1] * 20 + [90], [17 * i + 1 for i in range(20)] + [190], 0, False),
+]
+
+
+def _id(c):
+    return f"{c[0]}x{c[1]}x{c[2]}-page{c[3]}-{c[4]}-{c[5]}-{len(c[6])}r{sum(c[6])}t{max(c[7])}k-w{c[8]}{'-tm' if c[9] else ''}"
+
+
+def _attention_case(c, seed=0):
+    heads, kv_heads, dim, places, qt, kind, q_len, kv_len, window, tm = c
+    gen = _gen(seed)
+    pages = sum(-(-n // places) for n in kv_len) + 2
+    cache = _filled_cache(gen, pages, kv_heads, places, dim, kind, tm)
+    table, start, length = _batch(gen, q_len, kv_len, pages, places)
+    q = (2 * torch.randn((sum(q_len), heads, dim), generator=gen)).to(R.TYPES[qt])
+    return q, cache, table, start, length, window
+
+
+def _reference(q, cache, table, start, length, window, scale=None):
+    k, v, ke, ve = cache
+    ref, parts = R.attention(q.cpu().double().numpy(), R.cache_values(k, ke), R.cache_values(v, ve), table.numpy(), start.numpy(), length.numpy(),
+                             scale, window)
+    return ref, R.attention_bound(ref, parts, q.dtype, q.shape[2])
+
+
+def _close(got, ref, bound):
+    got = got.cpu().double().numpy()
+    assert np.isfinite(got).all()
+    over = np.abs(got - ref) - bound
+    at = np.unravel_index(over.argmax(), over.shape) if over.size else None
+    assert not over.size or over.max() <= 0, (at, got[at], ref[at], bound[at])
+
+
+@pytest.mark.parametrize("case", ATTENTION, ids=_id)
+def test_attention(case):
+    q, cache, table, start, length, window = _attention_case(case)
+    k, v, ke, ve = cache
+    status = I.new_status(DEV)
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, max_q=max(case[6]), window=window, status=status)
+    I.check(status)
+    _close(got, *_reference(q, cache, table, start, length, window))
+
+
+@pytest.mark.parametrize("case", ATTENTION[-4:], ids=_id)
+@pytest.mark.parametrize("max_q", [0, 1, 10 ** 6, None])
+def test_attention_whatever_the_host_expects(case, max_q):
+    q, cache, table, start, length, window = _attention_case(case, 1)
+    k, v, ke, ve = cache
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, max_q=max_q, window=window)
+    _close(got, *_reference(q, cache, table, start, length, window))
+
+
+def _random_case(seed):
+    rng = np.random.default_rng(seed)
+    kv_heads = int(rng.choice([1, 2, 3]))
+    group = int(rng.choice([1, 2, 3, 4, 5, 8, 16, 17]))
+    dim = int(rng.choice([64, 128, 256]))
+    qt = str(rng.choice(["bf16", "fp16"]))
+    kind = str(rng.choice([qt, "fp8"]))
+    n = int(rng.integers(1, 9))
+    q_len = [int(rng.choice([0, 1, 1, 1, 2, int(rng.integers(1, 20)), int(rng.integers(1, 150))])) for _ in range(n)]
+    kv_len = [int(max(0, q + rng.choice([-1, 0, 0, int(rng.integers(0, 40)), int(rng.integers(0, 900))]))) for q in q_len]
+    if sum(q_len) == 0:
+        q_len[0], kv_len[0] = 1, 3
+    window = int(rng.choice([0, 0, 0, 1, int(rng.integers(1, 200))]))
+    return (kv_heads * group, kv_heads, dim, int(rng.choice([1, 8, 16, 64, 256])), qt, kind, q_len, kv_len, window, bool(rng.random() < 0.4))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_attention_random_batches(seed):
+    case = _random_case(seed)
+    q, cache, table, start, length, window = _attention_case(case, seed)
+    k, v, ke, ve = cache
+    scale = None if seed % 3 else 0.11
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, max_q=max(case[6]), window=window, scale=scale)
+    _close(got, *_reference(q, cache, table, start, length, window, scale))
+
+
+def test_attention_long_decodes_are_split_and_joined():
+    # one and a few long requests on few kv heads: the keys of a row are shared out and the parts joined
+    for q_len, kv_len in (([1], [9001]), ([1, 1, 1], [4100, 1, 7000]), ([1, 40], [5000, 3000])):
+        case = (8, 1, 128, 64, "bf16", "bf16", q_len, kv_len, 0, False)
+        q, cache, table, start, length, window = _attention_case(case, 3)
+        got = I.attention(q.to(DEV), cache[0], cache[1], table.to(DEV), start.to(DEV), length.to(DEV), max_q=max(q_len))
+        _close(got, *_reference(q, cache, table, start, length, window))
+
+
+def test_attention_scores_far_apart():
+    # rows whose largest score lies in the last block of keys, in the first, and scores that are all far below zero
+    heads, dim = 4, 128
+    gen = _gen(5)
+    cache = _filled_cache(gen, 40, 1, 16, dim, "bf16")
+    table, start, length = _batch(gen, [1, 70], [300, 100], 40, 16)
+    q = (2 * torch.randn((71, heads, dim), generator=gen)).to(torch.bfloat16)
+    for scale in (3.0, -3.0, 1e-4, 0.0):
+        got = I.attention(q.to(DEV), cache[0], cache[1], table.to(DEV), start.to(DEV), length.to(DEV), scale=scale)
+        _close(got, *_reference(q, cache, table, start, length, 0, scale))
+
+
+# contents of places that no token sees: NaN, infinities and the type's lowest value, in keys and values
+@pytest.mark.parametrize("kind", ["bf16", "fp16", "fp8"])
+@pytest.mark.parametrize("poison", [float("nan"), float("inf"), -float("inf"), "lowest"])
+def test_attention_unseen_places_do_not_matter(kind, poison):
+    if kind == "fp8" and poison == -float("inf"):
+        pytest.skip("8 bits have no negative infinity")
+    qt = "bf16" if kind == "fp8" else kind
+    for case in ((8, 2, 128, 16, qt, kind, [1, 40, 130], [50, 45, 333], 0, False), (8, 2, 128, 16, qt, kind, [1, 40, 130], [50, 45, 333], 21, False)):
+        q, cache, table, start, length, window = _attention_case(case, 7)
+        ref = _reference(q, cache, table, start, length, window)
+        k, v, ke, ve = cache
+        value = torch.finfo(torch.bfloat16 if kind == "fp8" else R.TYPES[kind]).min if poison == "lowest" else poison
+        for t, e in ((k, ke), (v, ve)):
+            used = torch.zeros(t.shape[0] * t.shape[2], dtype=torch.bool)
+            for r, n in enumerate(case[7]):
+                for j in range(n):
+                    used[int(table[r, j // 16]) * 16 + j % 16] = True
+            free = (~used).view(t.shape[0], 16)
+            assert free.any()
+            pg, pl = free.nonzero(as_tuple=True)
+            if kind == "fp8":
+                b = t.view(torch.uint8)
+                b[pg.to(DEV), :, pl.to(DEV)] = 0xFE if poison == "lowest" else 0x7F
+                e[pg.to(DEV), :, pl.to(DEV)] = 254
+            else:
+                t[pg.to(DEV), :, pl.to(DEV)] = value
+        args = (k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve)
+        _close(I.attention(q.to(DEV), *args, window=window), *ref)
+        # the last token of the chunk's own cache (seen by the last token alone), then the first (out of most windows)
+        last = int(table[2, 332 // 16]), 332 % 16
+        first = int(table[2, 0]), 0
+        for page, place in (last, first):
+            for t, e in ((k, ke), (v, ve)):
+                if kind == "fp8":
+                    t.view(torch.uint8)[page, :, place] = 0xFE if poison == "lowest" else 0x7F
+                    e[page, :, place] = 254
+                else:
+                    t[page, :, place] = value
+        got = I.attention(q.to(DEV), *args, window=window).cpu().double().numpy()
+        sees = np.zeros(len(got), bool)
+        sees[-1] = True                                          # the last token sees its own place
+        if window == 0:
+            sees[41:] = True                                     # everyone in the chunk sees the first
+        elif 333 - 130 < window:
+            sees[41:41 + window] = True
+        over = np.abs(got - ref[0]) - ref[1]
+        assert np.isfinite(got[~sees]).all() and over[~sees].max() <= 0
+
+
+def test_attention_nan_that_is_seen_comes_out():
+    for q_len, kv_len in (([1], [40]), ([50], [60])):
+        case = (4, 2, 128, 16, "bf16", "bf16", q_len, kv_len, 0, False)
+        q, cache, table, start, length, _ = _attention_case(case, 11)
+        k, v = cache[0], cache[1]
+        j = 30
+        v[int(table[0, j // 16]), 1, j % 16, 5] = float("nan")
+        v[int(table[0, j // 16]), 1, j % 16, 6] = float("inf")
+        got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV)).cpu().double()
+        sees = np.arange(kv_len[0] - q_len[0], kv_len[0]) >= j
+        assert got[sees][:, 2:, 5].isnan().all() and (got[sees][:, 2:, 6] == float("inf")).all()
+        rest = got.clone()
+        rest[:, 2:, 5:7] = 0
+        assert rest.isfinite().all() and got[~sees].isfinite().all() and got[:, :2].isfinite().all()
+
+
+def test_attention_strides():
+    case = (8, 2, 128, 16, "bf16", "bf16", [1, 40, 1], [90, 55, 300], 0, False)
+    q, cache, table, start, length, _ = _attention_case(case, 13)
+    ref = _reference(q, cache, table, start, length, 0)
+    # q as a part of a projection's rows, out inside a larger tensor, the table with room to spare
+    wide = torch.zeros((42, 12, 128), dtype=torch.bfloat16, device=DEV)
+    wide[:, :8] = q.to(DEV)
+    room = torch.full((44, 9, 160), 7.0, dtype=torch.bfloat16, device=DEV)
+    out = room[1:43, :8, 16:144]
+    big = torch.zeros((3, 64), dtype=torch.int32, device=DEV)
+    big[:, :table.shape[1]] = table.to(DEV)
+    back = I.attention(wide[:, :8], cache[0], cache[1], big[:, :table.shape[1]], start.to(DEV), length.to(DEV), out=out)
+    assert back is out
+    _close(out, *ref)
+    room[1:43, :8, 16:144] = 7.0
+    assert (room == 7.0).all()
+
+
+def test_attention_offsets_beyond_32_bits():
+    # a cache whose later pages begin beyond 2^32 elements
+    places, heads, dim = 16, 1, 128
+    stride = 1 << 31
+    raw = torch.empty(2 * stride + places * dim + stride, dtype=torch.bfloat16, device=DEV)
+    k = raw.as_strided((3, heads, places, dim), (stride, places * dim, dim, 1))
+    v = raw.as_strided((3, heads, places, dim), (stride, places * dim, dim, 1), places * dim)
+    gen = _gen(17)
+    kk, vv = (torch.randn((3, heads, places, dim), generator=gen).to(torch.bfloat16) for _ in range(2))
+    slots = torch.arange(3 * places, device=DEV)
+    flat = lambda t: t.transpose(1, 2).reshape(-1, heads, dim).to(DEV)   # noqa: E731
+    I.kv_write(flat(kk), flat(vv), k, v, slots)
+    rk, rv = I.kv_read(k, v, slots)
+    assert torch.equal(rk, flat(kk)) and torch.equal(rv, flat(vv))
+    table = torch.tensor([[2, 0, 1], [1, 2, 0]], dtype=torch.int32)
+    start, length = torch.tensor([0, 1, 34], dtype=torch.int32), torch.tensor([48, 40], dtype=torch.int32)
+    q = torch.randn((34, 2, dim), generator=gen).to(torch.bfloat16)
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV))
+    ref, parts = R.attention(q.double().numpy(), kk.double().numpy(), vv.double().numpy(), table.numpy(), start.numpy(), length.numpy())
+    _close(got, ref, R.attention_bound(ref, parts, torch.bfloat16, dim))
+
+
+def test_attention_reports_numbers_out_of_range():
+    case = (4, 2, 128, 16, "bf16", "bf16", [1, 40, 2], [50, 60, 20], 0, False)
+    q, cache, table, start, length, _ = _attention_case(case, 19)
+    k, v = cache[0], cache[1]
+
+    def call(t=table, s=start, n=length):
+        status = I.new_status(DEV)
+        out = torch.zeros(q.shape, dtype=q.dtype, device=DEV)
+        I.attention(q.to(DEV), k, v, t.to(DEV), s.to(DEV), n.to(DEV), status=status, out=out)
+        word = int(status.item())
+        if word:
+            with pytest.raises(I.SimError):
+                I.check(status)
+        return word, out
+    assert call()[0] == 0
+    good = call()[1]
+    for bad in (-1, k.shape[0], 2 ** 31 - 1, -2 ** 31):
+        t = table.clone()
+        t[1, 1] = bad
+        word, out = call(t=t)
+        assert word == I.BAD_PAGE
+        assert torch.equal(out[0], good[0]) and torch.equal(out[41:], good[41:])          # other requests are as they were
+        keep = [j for j in range(60) if j // 16 != 1]                                     # the page's keys count as absent
+        t2 = table.clone()
+        kk, vv = (R.cache_values(c, None) for c in (k, v))
+        sub = np.concatenate([np.concatenate([kk[int(t2[1, p])] for p in range(4)], 1)[:, keep]])
+        subv = np.concatenate([np.concatenate([vv[int(t2[1, p])] for p in range(4)], 1)[:, keep]])
+        last = q[40].double().numpy()                                                     # the chunk's last token sees all that is kept
+        for h in range(4):
+            s = sub[h // 2] @ last[h] / np.sqrt(128)
+            w = np.exp(s - s.max())
+            ref = (w / w.sum()) @ subv[h // 2]
+            assert np.abs(out[40, h].cpu().double().numpy() - ref).max() < 0.05
+    word, out = call(n=torch.tensor([50, 1000, 20], dtype=torch.int32))                   # longer than its row of the table
+    assert word & I.BAD_BATCH and torch.equal(out[0], good[0]) and torch.equal(out[41:], good[41:])
+    assert call(n=torch.tensor([50, -3, 20], dtype=torch.int32))[0] & I.BAD_BATCH
+    for bad in ([0, 1, 41, 50], [0, 41, 1, 43], [-5, 1, 41, 43], [0, 1, 41, 30], [3, 2, 1, 0], [2 ** 31 - 1, -2 ** 31, 5, 43]):
+        assert call(s=torch.tensor(bad, dtype=torch.int32))[0] & I.BAD_BATCH, bad
+
+
+def test_attention_same_result_every_time_and_on_another_stream():
+    case = (8, 2, 128, 16, "bf16", "fp8", [1, 40, 1, 1], [3000, 900, 300, 1], 0, False)
+    q, cache, table, start, length, _ = _attention_case(case, 23)
+    k, v, ke, ve = cache
+    args = (k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve)
+    qq = q.to(DEV)
+    first = I.attention(qq, *args)
+    for _ in range(5):
+        assert torch.equal(I.attention(qq, *args), first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        other = I.attention(qq, *args)
+    side.synchronize()
+    assert torch.equal(other, first)
+
+
+def test_an_iteration_in_a_graph():
+    """Cache write, attention and adapters captured once and replayed as the requests grow, against eager calls."""
+    heads, kv_heads, dim, places, n = 8, 2, 128, 16, 5
+    gen = _gen(29)
+    pages = n * 8
+    k, v, ke, ve = I.new_cache(pages, kv_heads, places, dim, torch.float8_e4m3fn, DEV)
+    fill = torch.randn((n * 100, 2, kv_heads, dim), generator=gen).to(torch.bfloat16).to(DEV)
+    table = torch.randperm(pages, generator=gen).to(torch.int32).view(n, 8).to(DEV)
+
+    def slots_of(r, j):
+        return table[r, j // places].long() * places + j % places
+    lens = torch.tensor([30, 1, 64, 77, 16])
+    for r in range(n):
+        j = torch.arange(int(lens[r]), device=DEV)
+        I.kv_write(fill[r * 100:r * 100 + len(j), 0], fill[r * 100:r * 100 + len(j), 1], k, v, slots_of(r, j), ke, ve)
+    start = torch.arange(n + 1, dtype=torch.int32, device=DEV)
+    length, slots = lens.to(torch.int32).to(DEV), torch.zeros(n, dtype=torch.int64, device=DEV)
+    q, kn, vn = (torch.zeros(s, dtype=torch.bfloat16, device=DEV) for s in ((n, heads, dim), (n, kv_heads, dim), (n, kv_heads, dim)))
+    down = torch.randn((3, 16, heads * dim), generator=gen).to(torch.bfloat16).to(DEV) / 30
+    up = torch.randn((3, 256, 16), generator=gen).to(torch.bfloat16).to(DEV) / 4
+    scale, adapter = torch.tensor([1.0, 0.5, 2.0], device=DEV), torch.tensor([0, 2, -1, 0, 1], dtype=torch.int32, device=DEV)
+    base = torch.randn((n, 256), generator=gen).to(torch.bfloat16).to(DEV)
+
+    def step():
+        I.kv_write(kn, vn, k, v, slots, ke, ve)
+        o = I.attention(q, k, v, table, start, length, ke, ve, max_q=1)
+        return o, I.adapters(o.view(n, heads * dim), base, down, up, scale, start, adapter)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        slots.fill_(-1)
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    for i in range(6):
+        for r in range(n):
+            slots[r] = slots_of(r, lens[r].to(DEV))
+        lens += 1
+        length.copy_(lens.to(torch.int32))
+        for t in (q, kn, vn):
+            t.copy_(torch.randn(t.shape, generator=gen).to(torch.bfloat16))
+        graph.replay()
+        got = [t.clone() for t in out]
+        torch.cuda.synchronize()
+        want = step()
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+
+
+# ---- the cache
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("kind,qt", [("bf16", "bf16"), ("fp16", "fp16"), ("fp8", "bf16"), ("fp8", "fp16")])
+@pytest.mark.parametrize("tokens,heads,places,tm", [(1, 1, 16, False), (37, 3, 16, True), (130, 2, 1, False), (64, 2, 128, False)])
+def test_cache_write_and_read(dim, kind, qt, tokens, heads, places, tm):
+    gen = _gen(tokens + dim)
+    pages = -(-tokens // places) + 2
+    k, v, ke, ve = _filled_cache(gen, pages, heads, places, dim, kind, tm)
+    before = [R.cache_values(t, e) for t, e in ((k, ke), (v, ve))]
+    order = torch.randperm(pages * places, generator=gen)[:tokens].to(DEV)
+    rows = torch.randn((tokens, 2, heads + 1, dim), generator=gen) * torch.exp(3 * torch.randn((tokens, 2, heads + 1, 1), generator=gen))
+    rows[0, 0, 0, 1:] = 0
+    rows[-1, 1, 0] = 0
+    rows = rows.to(R.TYPES[qt])
+    new = rows.to(DEV)[:, :, :heads]                            # strided: part of a projection's output
+    I.kv_write(new[:, 0], new[:, 1], k, v, order, ke, ve)
+    got = I.kv_read(k, v, order, ke, ve, dtype=R.TYPES[qt])
+    for i, (t, e) in enumerate(((k, ke), (v, ve))):
+        x = rows[:, i, :heads].double().numpy()
+        values = R.cache_values(t, e)
+        at = np.asarray(order.cpu())
+        stored = values[at // places, :, at % places]
+        if kind == "fp8":
+            code, ex = R.quantise(x)
+            assert np.array_equal(e.cpu().numpy()[at // places, :, at % places].astype(int) - 127, ex)
+            assert np.array_equal(stored, code * 2.0 ** ex[..., None])
+        else:
+            assert np.array_equal(stored, x)
+        assert np.array_equal(got[i].cpu().double().numpy(), torch.from_numpy(stored).to(R.TYPES[qt]).double().numpy())
+        rest = np.ones((pages, places), bool)
+        rest[at // places, at % places] = False
+        pg, pl = rest.nonzero()
+        assert np.array_equal(values[pg, :, pl], before[i][pg, :, pl])     # nothing else is touched
+
+
+@pytest.mark.parametrize("qt", ["bf16", "fp16"])
+def test_quantising_every_kind_of_row(qt):
+    """Rows at the borders: powers of two, 448 times them and the next value above, subnormal numbers, the largest ones, ties,
+    zeros of both signs, NaN and infinities."""
+    t = R.TYPES[qt]
+    info = torch.finfo(t)
+    tops = [448.0, 1.75, 3.5, 1.0, 2.0, info.max, info.smallest_normal, info.smallest_normal * info.eps, info.tiny * 3, 0.0]
+    tops += [float(torch.nextafter(torch.tensor(x, dtype=t), torch.tensor(info.max, dtype=t))) for x in (448.0, 1.75, 224.0, 0.875)]
+    ramp = torch.cat([torch.linspace(-1, 1, 57), torch.tensor([0.0, -0.0, 2.0 ** -9, 2.0 ** -10, 3 * 2.0 ** -10, 17 / 448, 2.0 ** -20])])
+    rows = torch.stack([(ramp.double() * x).to(t) for x in tops])
+    rows[:, 0] = torch.tensor(tops).to(t)
+    bad = rows[:3].clone()
+    bad[0, 5], bad[1, 6], bad[2, 63] = float("nan"), float("inf"), -float("inf")
+    rows = torch.cat([rows, bad])
+    n = len(rows)
+    k, v, ke, ve = I.new_cache(n, 1, 1, 64, torch.float8_e4m3fn, DEV)
+    slots = torch.arange(n, device=DEV)
+    x = rows.view(n, 1, 64).to(DEV)
+    I.kv_write(x, x, k, v, slots, ke, ve)
+    code, ex = R.quantise(rows.double().numpy())
+    for c, e in ((k, ke), (v, ve)):
+        assert np.array_equal(e.cpu().numpy().reshape(n).astype(int) - 127, ex)
+        got = R.E4M3[c.view(torch.uint8).cpu().numpy()].reshape(n, 64)
+        assert np.array_equal(got, code, equal_nan=True)
+    back = I.kv_read(k, v, slots, ke, ve, dtype=t)[0].cpu().view(n, 64)
+    want = torch.from_numpy(code * 2.0 ** ex[:, None]).to(t)
+    assert torch.equal(torch.isnan(back), torch.isnan(want)) and torch.equal(back.nan_to_num(), want.nan_to_num())
+    assert torch.isnan(back[-3:]).all()
+
+
+def test_slots_outside_the_cache_are_no_place():
+    for kind in ("bf16", "fp8"):
+        k, v, ke, ve = _filled_cache(_gen(3), 4, 2, 16, 128, kind)
+        before = [None if t is None else t.clone() for t in (k, v, ke, ve)]
+        slots = torch.tensor([-1, 64, 2 ** 40, -2 ** 62, 5], device=DEV)
+        x = torch.randn((5, 2, 128), generator=_gen(4)).to(torch.bfloat16).to(DEV)
+        I.kv_write(x, x, k, v, slots, ke, ve)
+        for a, b in zip((k, v, ke, ve), before):
+            if a is not None:
+                d = (a.view(torch.uint8) != b.view(torch.uint8)).view(4, 2, 16, -1).any(-1).any(1)
+                assert not d[1:].any() and d[0].sum() <= 1 and not d[0, :5].any()
+        rk, rv = I.kv_read(k, v, slots, ke, ve)
+        assert (rk[:4] == 0).all() and (rv[:4] == 0).all() and (rk[4] != 0).any()
+    e = torch.zeros(0, dtype=torch.int64, device=DEV)
+    I.kv_write(x[:0], x[:0], k, v, e, ke, ve)
+    assert I.kv_read(k, v, e, ke, ve)[0].shape == (0, 2, 128)
+
+
+# ---- adapters
+
+# (type, rank, width in, width out, adapters, tokens of each request, adapter of each request)
+ADAPTERS = [
+    ("bf16", 8, 8, 8, 1, [1], [0]),
+    ("bf16", 16, 4096, 256, 3, [1, 1, 1, 1], [0, 2, -1, 2]),
+    ("fp16", 64, 520, 1032, 8, [1, 30, 1, 0, 70, 1], [7, 3, 0, 1, 3, -1]),
+    ("bf16", 32, 1024, 768, 2, [200], [1]),
+    ("fp16", 128, 136, 264, 4, [17, 33, 1], [0, 0, 3]),
+    ("bf16", 24, 2056, 72, 5, [1] * 70, [i % 6 - 1 for i in range(70)]),
+    ("fp16", 40, 264, 2000, 300, [1] * 40 + [65], list(range(0, 280, 7)) + [299]),
+    ("bf16", 56, 72, 520, 2, [129, 64, 63, 1], [0, -1, 1, 0]),
+    ("fp16", 8, 8000, 8, 2, [5, 1], [-1, -1]),
+]
+
+
+def _adapter_case(c, seed=0):
+    t, rank, wi, wo, n, q_len, which = c
+    g = _gen(seed)
+    t = R.TYPES[t]
+    T = sum(q_len)
+    x = torch.randn((T, wi), generator=g).to(t)
+    base = torch.randn((T, wo), generator=g).to(t)
+    down = (torch.randn((n, rank, wi), generator=g) / wi ** 0.5).to(t)
+    up = (torch.randn((n, wo, rank), generator=g) / rank ** 0.5).to(t)
+    scale = torch.rand(n, generator=g) + 0.5
+    start = torch.tensor(np.concatenate([[0], np.cumsum(q_len)]).astype(np.int32))
+    return x, base, down, up, scale, start, torch.tensor(which, dtype=torch.int32)
+
+
+def _adapters_close(got, case):
+    x, base, down, up, scale, start, which = case
+    d = [t.double().numpy() for t in (x, base, down, up, scale)]
+    ref, inner, outer = R.adapters(*d, start.numpy(), which.numpy())
+    bound = R.adapters_bound(ref, d[1], inner, outer, x.dtype, x.shape[1], down.shape[1])
+    _close(got, ref, bound)
+    for r, a in enumerate(which.tolist()):
+        if a < 0:
+            s = slice(int(start[r]), int(start[r + 1]))
+            assert torch.equal(got[s].cpu(), base[s])            # nothing is added: the same bits
+
+
+@pytest.mark.parametrize("case", ADAPTERS, ids=lambda c: f"{c[0]}-r{c[1]}-{c[2]}x{c[3]}-{c[4]}a-{sum(c[5])}t")
+def test_adapters(case):
+    data = _adapter_case(case)
+    status = I.new_status(DEV)
+    dev = [t.to(DEV) for t in data]
+    got = I.adapters(*dev, status=status)
+    I.check(status)
+    _adapters_close(got, data)
+    again = I.adapters(*dev)
+    assert torch.equal(again, got)
+    out = dev[1].clone()                                         # in place
+    assert I.adapters(dev[0], out, *dev[2:], out=out) is out
+    assert torch.equal(out, got)
+
+
+def test_adapters_strides_and_large_numbers():
+    case = list(_adapter_case(("fp16", 16, 256, 512, 2, [3, 40], [1, 0]), 5))
+    case[0] = (case[0] * 200).half()                             # inner products beyond fp16's range, an adapter scale that brings them back
+    case[2] = (case[2] * 100).half()
+    case[4] = case[4] * 1e-4
+    dev = [t.to(DEV) for t in case]
+    wide_x = torch.zeros((43, 300 + 4), dtype=torch.float16, device=DEV)
+    wide_x[:, 8:264] = dev[0]
+    wide_b = torch.zeros((43, 1024), dtype=torch.float16, device=DEV)
+    wide_b[:, :512] = dev[1]
+    room = torch.full((43, 640), 3.0, dtype=torch.float16, device=DEV)
+    out = room[:, 64:576]
+    I.adapters(wide_x[:, 8:264], wide_b[:, :512], *dev[2:], out=out)
+    _adapters_close(out, case)
+    room[:, 64:576] = 3.0
+    assert (room == 3.0).all()
+    tiny = list(_adapter_case(("fp16", 16, 256, 512, 2, [3, 40], [1, 0]), 6))
+    tiny[2] = (tiny[2] * 1e-5).half()                            # inner products below fp16's smallest numbers, brought back by the scale
+    tiny[4] = tiny[4] * 1e5
+    _adapters_close(I.adapters(*[t.to(DEV) for t in tiny]), tiny)
+
+
+def test_adapters_infinities_stay_in_their_rows():
+    data = _adapter_case(("bf16", 16, 256, 512, 2, [1, 30, 1], [1, 0, 1]), 9)
+    dev = [t.to(DEV) for t in data]
+    good = I.adapters(*dev)
+    x = dev[0].clone()
+    x[7, 3], x[9, 5] = float("nan"), float("inf")
+    got = I.adapters(x, *dev[1:])
+    rows = [i for i in range(32) if i not in (7, 9)]
+    assert torch.equal(got[rows], good[rows]) and got[7].isnan().all() and not got[9].isfinite().any()
+
+
+def test_adapters_report_numbers_out_of_range():
+    data = _adapter_case(("bf16", 16, 256, 512, 2, [1, 30, 1], [1, 0, 1]), 10)
+    dev = [t.to(DEV) for t in data]
+    good = I.adapters(*dev)
+    for bad in (2, -2, 2 ** 31 - 1, -2 ** 31):
+        which = dev[6].clone()
+        which[1] = bad
+        status = I.new_status(DEV)
+        got = I.adapters(*dev[:6], which, status=status)
+        assert int(status.item()) == I.BAD_ADAPTER
+        assert torch.equal(got[0], good[0]) and torch.equal(got[31], good[31]) and torch.equal(got[1:31], dev[1][1:31])
+    for bad in ([0, 1, 31, 50], [0, 31, 1, 32], [-5, 1, 31, 32], [0, 1, 31, 20], [2 ** 31 - 1, -2 ** 31, 5, 32]):
+        status = I.new_status(DEV)
+        I.adapters(*dev[:5], torch.tensor(bad, dtype=torch.int32, device=DEV), dev[6], status=status)
+        assert int(status.item()) & I.BAD_BATCH, bad
+    none = I.adapters(dev[0], dev[1], dev[2][:0], dev[3][:0], dev[4][:0], dev[5], torch.full_like(dev[6], -1))
+    assert torch.equal(none, dev[1])                             # no adapter loaded
