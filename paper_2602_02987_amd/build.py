@@ -17,6 +17,7 @@ SOURCES = ["gnr_kernels.hip", "gnr_api.cpp", "gnr_tables.cpp"] + [f"gnr_step_{v}
 # the operators of a batch iteration
 ITER_SOURCES = ["gnr_iter_api.cpp", "gnr_iter_cache.hip", "gnr_iter_attention.hip", "gnr_iter_adapters.hip"]
 ITER_HEADERS = [os.path.join(CSRC_ITER, "gnr_iter_internal.h"), os.path.join(CSRC_ITER, "gnr_iter_device.h"),
+                os.path.join(CSRC_ITER, "gnr_iter_attention.h"),
                 os.path.join(INCLUDE, "gnr_iter.h"), os.path.join(INCLUDE, "gnr_sim.h")]
 HEADERS = [os.path.join(CSRC, "gnr_step.h"), os.path.join(CSRC, "gnr_internal.h"), os.path.join(INCLUDE, "gnr_sim.h")]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")

@@ -119,7 +119,6 @@ int iter_attention(const iter_cache *c, const iter_batch *b, int type, int heads
   p.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
   p.window = window;
   p.workspace = static_cast<float *>(workspace);
-  p.bytes = bytes;
   p.status = status;
   return launch_attention(p, hip_stream);
 }

@@ -35,6 +35,8 @@ struct Bf16 {
   static constexpr uint32_t kInf = 0x7F80u;
   static __device__ __forceinline__ float widen(uint32_t w) { return bits<float>(w << 16); }
   static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<__bf16>(a), static_cast<__bf16>(b)}; return bits<uint32_t>(p); }
+  static __device__ __forceinline__ f32x4 mfma16(oct a, oct b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mfma32(oct a, oct b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   template <bool kUpper>
   static __device__ __forceinline__ uint32_t from_e4m3(uint32_t codes, float scale) { return bits<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, kUpper)); }
   template <bool kUpper>
@@ -47,6 +49,8 @@ struct Fp16 {
   static constexpr uint32_t kInf = 0x7C00u;
   static __device__ __forceinline__ float widen(uint32_t w) { return static_cast<float>(bits<_Float16>(static_cast<uint16_t>(w))); }
   static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<_Float16>(a), static_cast<_Float16>(b)}; return bits<uint32_t>(p); }
+  static __device__ __forceinline__ f32x4 mfma16(oct a, oct b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
+  static __device__ __forceinline__ f32x16 mfma32(oct a, oct b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   template <bool kUpper>
   static __device__ __forceinline__ uint32_t from_e4m3(uint32_t codes, float scale) { return bits<uint32_t>(__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(codes, scale, kUpper)); }
   template <bool kUpper>

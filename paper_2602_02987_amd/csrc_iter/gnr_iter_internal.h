@@ -18,7 +18,7 @@ struct AttentionParams {
   float scale_log2;            // scale / ln 2: weights are powers of two
   int64_t window;
   float *workspace;
-  size_t bytes;
+  int64_t header;              // words of the workspace before the parts
   uint32_t *status;
 };
 
