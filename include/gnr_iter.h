@@ -27,14 +27,14 @@
 extern "C" {
 #endif
 
-#define ITER_MAX_REQUESTS 4096  /* requests of one batch */
+#define ITER_MAX_REQUESTS 1024  /* requests of one batch */
 #define ITER_MAX_ADAPTERS 4096  /* adapters loaded */
 #define ITER_MAX_RANK 128
 
 /* Element types. FP8 (e4m3: 4 exponent bits, 3 of mantissa, largest value 448, no infinity) is a cache type only. */
 enum iter_type { ITER_BF16 = 0, ITER_FP16 = 1, ITER_FP8 = 2 };
 
-/* BATCH: q_start does not ascend within [0, tokens], or a kv_len is negative or longer than its row of the page table.
+/* BATCH: q_start does not ascend within [0, tokens], or a kv_len is negative or longer than its row of the page table (or 2^30).
  * PAGE: a page number outside the cache. ADAPTER: an adapter number outside [-1, adapters). */
 enum iter_status { ITER_BAD_BATCH = 1, ITER_BAD_PAGE = 2, ITER_BAD_ADAPTER = 4 };
 
@@ -97,7 +97,7 @@ int iter_attention_bytes(const iter_cache *cache, const iter_batch *batch, int h
  * h / (heads / kv_heads). The token at position p = kv_len - q_len + i of its request sees positions max(0, p - window + 1) .. p
  * (window = 0: 0 .. p): out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q.k_j). A token that sees nothing gets zeros. What lies
  * where a token does not look (NaN included) does not matter. Scores, sums and outputs are held in 32 bits; the weights are rounded to `type` for
- * the matrix product with the values, relative to the largest of their row. Rows of tokens outside every request are not written. */
+ * the matrix product with the values, relative to the largest of their row. Rows of tokens outside every request are not written. out must not overlap q. */
 int iter_attention(const iter_cache *cache, const iter_batch *batch, int type, int heads, const iter_rows *q,
                    const iter_rows *out, double scale, int64_t window, void *workspace, size_t bytes, uint32_t *status,
                    void *hip_stream);

@@ -15,7 +15,8 @@ OBJ = os.path.join(HERE, "_build")
 STEP_VARIANTS = ["plain", "rr", "im", "ab", "ab_rr", "ab_im", "ws"]
 SOURCES = ["gnr_kernels.hip", "gnr_api.cpp", "gnr_tables.cpp"] + [f"gnr_step_{v}.hip" for v in STEP_VARIANTS]
 # the operators of a batch iteration
-ITER_SOURCES = ["gnr_iter_api.cpp", "gnr_iter_cache.hip", "gnr_iter_attention.hip", "gnr_iter_adapters.hip"]
+ITER_SOURCES = ["gnr_iter_api.cpp", "gnr_iter_cache.hip", "gnr_iter_attention.hip",
+                "gnr_iter_attention_rows.hip", "gnr_iter_attention_chunk.hip", "gnr_iter_adapters.hip"]
 ITER_HEADERS = [os.path.join(CSRC_ITER, "gnr_iter_internal.h"), os.path.join(CSRC_ITER, "gnr_iter_device.h"),
                 os.path.join(CSRC_ITER, "gnr_iter_attention.h"),
                 os.path.join(INCLUDE, "gnr_iter.h"), os.path.join(INCLUDE, "gnr_sim.h")]

@@ -1,6 +1,7 @@
 // Host side of the iteration operators: argument checks, nothing else.
 #include <cmath>
 #include <cstdint>
+#include <initializer_list>
 
 #include "gnr_iter_internal.h"
 
@@ -117,7 +118,7 @@ int iter_attention(const iter_cache *c, const iter_batch *b, int type, int heads
   p.type = type; p.heads = heads; p.group = heads / c->kv_heads;
   p.page_shift = __builtin_ctz(static_cast<unsigned>(c->page));
   p.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
-  p.window = window;
+  p.window = static_cast<int>(window < (int64_t(1) << 30) ? window : 0);   // no request is longer
   p.workspace = static_cast<float *>(workspace);
   p.status = status;
   return launch_attention(p, hip_stream);

@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "gnr_iter_internal.h"
 
 namespace gnr {
@@ -14,6 +16,7 @@ typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(2))) short s16x2;
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(8))) short s16x8;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
@@ -58,6 +61,23 @@ struct Fp16 {
 };
 
 __device__ __forceinline__ float exponent_scale(uint32_t byte) { return bits<float>(byte << 23); }
+
+// Whether either of two 16-bit values is a NaN or an infinity.
+template <class T>
+__device__ __forceinline__ bool no_number(uint32_t w) { return (w & T::kInf) == T::kInf || (w >> 16 & T::kInf) == T::kInf; }
+
+// A wave's load of 64 x 16 bytes from memory to 1 KB of shared memory, lane after lane; wait_for_lds_loads waits for all of the wave's.
+__device__ __forceinline__ void load_to_lds(const void *from, char *to)
+{
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)from, (__attribute__((address_space(3))) void *)to, 16, 0, 0);
+}
+__device__ __forceinline__ void wait_for_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Transposing LDS load: of 16 lanes, lanes 4 r to 4 r + 3 point at row r of a matrix of 4 x 16 16-bit elements; lane i gets column i.
+__device__ __forceinline__ s16x4 read_transposed(const char *at)
+{
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4 *)at);
+}
 
 inline int iter_hip_ok(hipError_t e) { return e == hipSuccess ? SIM_OK : SIM_EHIP; }
 

@@ -16,9 +16,12 @@ struct AttentionParams {
   int type, heads, group;      // group: query heads to a kv head
   int page_shift;
   float scale_log2;            // scale / ln 2: weights are powers of two
-  int64_t window;
+  int window, room;            // room: the most keys a request can have
   float *workspace;
-  int64_t header;              // words of the workspace before the parts
+  // of the kernel for few rows (0) and the one for chunks (1): rows of the requests it takes, workgroups, first word of its parts
+  int least[2], most[2], blocks[2];
+  int64_t parts[2];
+  int64_t marks[2], units[2];  // first word of the units' marks and how many there can be
   uint32_t *status;
 };
 

@@ -110,7 +110,7 @@ def test_attention_calls_that_are_refused():
         assert _attend(_cache(**bad)) == EINVAL
     for bad in BAD_PLANES:
         assert _attend(_plane(_cache(), **bad)) == EINVAL
-    for bad in (dict(requests=-1), dict(requests=4097), dict(tokens=-1), dict(tokens=1 << 31), dict(max_q=-1), dict(q_start=None), dict(kv_len=None),
+    for bad in (dict(requests=-1), dict(requests=1025), dict(tokens=-1), dict(tokens=1 << 31), dict(max_q=-1), dict(q_start=None), dict(kv_len=None),
                 dict(page_table=None), dict(table_stride=-1), dict(table_width=-1), dict(table_width=1 << 31)):
         assert _attend(batch=_batch(**bad)) == EINVAL, bad
     assert _attend(heads=3) == EINVAL and _attend(heads=0) == EINVAL and _attend(heads=8192) == EINVAL
@@ -136,7 +136,7 @@ def _adapt(typ=0, requests=2, tokens=5, q_start=P, adapter=P, x=P, xs=64, base=P
 def test_adapter_calls_that_are_refused():
     for bad in (dict(adapters=-1), dict(adapters=4097), dict(rank=0), dict(rank=12), dict(rank=136), dict(width_in=60), dict(width_in=0),
                 dict(width_out=4), dict(width_out=130), dict(down=None), dict(up=None), dict(up=P + 8), dict(scale=None), dict(typ=2), dict(typ=-1),
-                dict(requests=-1), dict(requests=4097), dict(tokens=-1), dict(q_start=None), dict(adapter=None), dict(x=None), dict(x=P + 2),
+                dict(requests=-1), dict(requests=1025), dict(tokens=-1), dict(q_start=None), dict(adapter=None), dict(x=None), dict(x=P + 2),
                 dict(base=None), dict(out=None), dict(xs=60), dict(bs=-128), dict(os_=132)):
         assert _adapt(**bad) == EINVAL, bad
     need = C.c_size_t(0)
