@@ -28,7 +28,7 @@ extern "C" {
 #endif
 
 #define ITER_MAX_REQUESTS 1024  /* requests of one batch */
-#define ITER_MAX_ADAPTERS 4096  /* adapters loaded */
+#define ITER_MAX_ADAPTERS 2048  /* adapters loaded */
 #define ITER_MAX_RANK 128
 
 /* Element types. FP8 (e4m3: 4 exponent bits, 3 of mantissa, largest value 448, no infinity) is a cache type only. */

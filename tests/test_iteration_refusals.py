@@ -134,7 +134,7 @@ def _adapt(typ=0, requests=2, tokens=5, q_start=P, adapter=P, x=P, xs=64, base=P
 
 
 def test_adapter_calls_that_are_refused():
-    for bad in (dict(adapters=-1), dict(adapters=4097), dict(rank=0), dict(rank=12), dict(rank=136), dict(width_in=60), dict(width_in=0),
+    for bad in (dict(adapters=-1), dict(adapters=2049), dict(rank=0), dict(rank=12), dict(rank=136), dict(width_in=60), dict(width_in=0),
                 dict(width_out=4), dict(width_out=130), dict(down=None), dict(up=None), dict(up=P + 8), dict(scale=None), dict(typ=2), dict(typ=-1),
                 dict(requests=-1), dict(requests=1025), dict(tokens=-1), dict(q_start=None), dict(adapter=None), dict(x=None), dict(x=P + 2),
                 dict(base=None), dict(out=None), dict(xs=60), dict(bs=-128), dict(os_=132)):
