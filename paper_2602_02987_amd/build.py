@@ -10,6 +10,8 @@ CSRC = os.path.join(HERE, "csrc")
 CSRC_ITER = os.path.join(HERE, "csrc_iter")
 INCLUDE = os.path.join(os.path.dirname(HERE), "include")
 LIB = os.path.join(HERE, "libgnr_sim.so")
+# the iteration operators' binding, which handles torch tensors in compiled code
+BINDING = os.path.join(HERE, "_iteration.so")
 OBJ = os.path.join(HERE, "_build")
 # every policy variant of the step kernel is a translation unit of its own, so that they compile side by side
 STEP_VARIANTS = ["plain", "rr", "im", "ab", "ab_rr", "ab_im", "ws"]
@@ -74,7 +76,28 @@ def build(verbose: bool = False, force: bool = True, jobs: int | None = None) ->
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
+    build_binding(verbose, force)
     return LIB
+
+
+def build_binding(verbose: bool = False, force: bool = True) -> str:
+    """Compiles the iteration operators' binding against the library and the torch that is installed (host code only)."""
+    import importlib.util
+    import sysconfig
+    src = os.path.join(CSRC_ITER, "gnr_iter_python.cpp")
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    deps = [src, os.path.join(INCLUDE, "gnr_iter.h"), os.path.join(torch, "version.py")]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) > os.path.getmtime(d) for d in deps):
+        return BINDING
+    headers = [os.path.join(torch, "include"), os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+               os.path.join(os.path.dirname(os.path.dirname(HIPCC)), "include"), sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM"]
+    cmd += [f"-isystem{h}" for h in headers] + [f"-I{INCLUDE}", src, "-o", BINDING, f"-L{HERE}", "-l:libgnr_sim.so", "-Wl,-rpath,$ORIGIN"]
+    cmd += [f"-L{os.path.join(torch, 'lib')}"] + [f"-l{n}" for n in ("c10", "c10_hip", "torch_cpu", "torch_python")]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
+    return BINDING
 
 
 def lib_path() -> str:
