@@ -488,6 +488,8 @@ ADAPTERS = [
     ("fp16", 40, 264, 2000, 300, [1] * 40 + [65], list(range(0, 280, 7)) + [299]),
     ("bf16", 56, 72, 520, 2, [129, 64, 63, 1], [0, -1, 1, 0]),
     ("fp16", 8, 8000, 8, 2, [5, 1], [-1, -1]),
+    ("bf16", 40, 264, 520, 3, [1] * 30 + [2100], [i % 4 - 1 for i in range(30)] + [2]),     # many tokens: larger tiles
+    ("fp16", 128, 1032, 776, 2, [1000, 1, 1500, 3], [1, 0, -1, 1]),
 ]
 
 
