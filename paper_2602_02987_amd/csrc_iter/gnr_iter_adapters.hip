@@ -152,14 +152,14 @@ __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const Adapt
 
 // out = base + scale up h of a tile, 128 columns to a wave: Y^T = up H^T with 16 rows of up at a time as the left operand. h is in 32 bits; it goes
 // into the product as the sum of two 16-bit numbers, relative to a power of two near the token's largest, so that neither type's range nor
-// its precision shows. The rows of up that a product takes are chosen so that a lane ends up with 32 neighbouring columns of its token: base
-// and out are read and written 16 bytes at a time. Bound by these two; for few tokens by latency, so base and the rows of up are asked for
+// its precision shows. The rows of up that two products take are chosen so that a lane ends up with eight neighbouring columns of its token, and the four
+// lanes of a token with 32: base and out are read and written 16 bytes a lane, 64 a token. Bound by these two; for few tokens by latency, so base and the rows of up are asked for
 // before h is added up.
 template <class T, int kRankSteps, int kSub>
 __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapters_up_kernel(const AdapterParams p, int splits)
 {
   typedef typename T::oct oct;
-  constexpr int kTile = 16 * kSub, kProducts = kColumns / 16, kRun = kColumns / 4, kPitch = kRankSteps * 32 + 4;
+  constexpr int kTile = 16 * kSub, kProducts = kColumns / 16, kLoads = kColumns / 32, kPitch = kRankSteps * 32 + 4;
   extern __shared__ int numbers[];
   __shared__ int tokens[kTile];
   __shared__ __attribute__((aligned(16))) float h[kTile][kPitch];
@@ -168,14 +168,14 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
   const bool none = which == p.set.adapters;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = lane % 16, g = lane / 16;
   const int rank = p.set.rank, width = static_cast<int>(p.set.width_out);
-  const int column0 = (blockIdx.y * kWaves + wave) * kColumns, column = column0 + g * kRun;
-  u32x4 y[kRun / 8];
+  const int column0 = (blockIdx.y * kWaves + wave) * kColumns, column = column0 + 8 * g;   // (and 32 on for the next load)
+  u32x4 y[kLoads];
   const auto load_base = [&](int s) {
     const int token = tokens[16 * s + n];
     const uint16_t *base = static_cast<const uint16_t *>(p.base) + static_cast<int64_t>(max(token, 0)) * p.base_stride;
 #pragma unroll
-    for (int j = 0; j < kRun / 8; ++j)
-      if (column + 8 * j < width) y[j] = *reinterpret_cast<const u32x4 *>(base + column + 8 * j);
+    for (int j = 0; j < kLoads; ++j)
+      if (column + 32 * j < width) y[j] = *reinterpret_cast<const u32x4 *>(base + column + 32 * j);
   };
   load_base(0);
   u32x4 rows[kRankSteps][kProducts];
@@ -186,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
     for (int i = 0; i < kRankSteps; ++i)
 #pragma unroll
       for (int j = 0; j < kProducts; ++j) {
-        const int row = column0 + n / 4 * kRun + 4 * j + n % 4, r = 32 * i + 8 * g;
+        const int row = column0 + 32 * (j / 2) + 8 * (n / 4) + 4 * (j % 2) + n % 4, r = 32 * i + 8 * g;
         rows[i][j] = u32x4{0, 0, 0, 0};
         if (row < width && r < rank) rows[i][j] = *reinterpret_cast<const u32x4 *>(up + static_cast<int64_t>(row) * rank + r);
       }
@@ -249,9 +249,9 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
       }
     }
     uint16_t *out = static_cast<uint16_t *>(p.out) + static_cast<int64_t>(max(token, 0)) * p.out_stride;
-    u32x4 z[kRun / 8];
+    u32x4 z[kLoads];
 #pragma unroll
-    for (int j = 0; j < kRun / 8; ++j) {
+    for (int j = 0; j < kLoads; ++j) {
       z[j] = y[j];
       if (!none) {
 #pragma unroll
@@ -263,8 +263,8 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
     }
     if (s + 1 < kSub) load_base(s + 1);
 #pragma unroll
-    for (int j = 0; j < kRun / 8; ++j)
-      if (token >= 0 && column + 8 * j < width) *reinterpret_cast<u32x4 *>(out + column + 8 * j) = z[j];
+    for (int j = 0; j < kLoads; ++j)
+      if (token >= 0 && column + 32 * j < width) *reinterpret_cast<u32x4 *>(out + column + 32 * j) = z[j];
   }
 }
 
