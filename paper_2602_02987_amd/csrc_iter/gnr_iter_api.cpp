@@ -10,6 +10,7 @@ namespace {
 
 constexpr int64_t kMaxTokens = int64_t(1) << 30;
 constexpr int64_t kMaxStride = int64_t(1) << 40;
+constexpr int64_t kMaxPlaceStride = int64_t(1) << 24;   // (sixteen of them are an offset of 32 bits)
 constexpr int kMaxHeads = 4096;
 
 bool aligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
@@ -28,7 +29,7 @@ bool span_ok(int64_t n, int64_t stride) { return n <= 0 || stride <= (int64_t(1)
 bool plane_ok(const iter_cache &c, const iter_plane &p)
 {
   const int size = c.type == ITER_FP8 ? 1 : 2;
-  if (!strides_ok(size, p.page_stride, p.head_stride, p.place_stride) || !span_ok(c.pages, p.page_stride)) return false;
+  if (!strides_ok(size, p.page_stride, p.head_stride, p.place_stride) || !span_ok(c.pages, p.page_stride) || p.place_stride > kMaxPlaceStride) return false;
   if (c.pages > 0 && (!p.data || !aligned(p.data))) return false;
   if (c.type != ITER_FP8) return p.exp == nullptr;
   for (const int64_t s : {p.exp_page_stride, p.exp_head_stride, p.exp_place_stride})
@@ -117,7 +118,9 @@ int iter_attention(const iter_cache *c, const iter_batch *b, int type, int heads
   p.cache = *c; p.batch = *b; p.q = *q; p.out = *out;
   p.type = type; p.heads = heads; p.group = heads / c->kv_heads;
   p.page_shift = __builtin_ctz(static_cast<unsigned>(c->page));
-  p.scale_log2 = static_cast<float>(scale * 1.4426950408889634);
+  // (its sign goes into the queries; a scale of zero is a tiny one, so that a hidden key's score of -infinity stays what it is)
+  p.scale_log2 = static_cast<float>(std::fmax(std::fabs(scale * 1.4426950408889634), 1e-30));
+  p.flip = scale < 0.0 ? 0x80008000u : 0u;
   p.window = static_cast<int>(window < (int64_t(1) << 30) ? window : 0);   // no request is longer
   p.workspace = static_cast<float *>(workspace);
   p.status = status;

@@ -34,7 +34,7 @@ __device__ __forceinline__ void one_row(const AttentionParams &p, int r, const R
       const float scale = fp8 ? exponent_scale(k.exp[page * k.exp_page_stride + head * k.exp_head_stride + place * k.exp_place_stride]) : 1.0f;
       float dot = 0.0f;
       for (int d = 0; d < kDim; ++d) dot = __builtin_fmaf(element(k, at + d, scale), T::widen(q[d]), dot);
-      s = dot * p.scale_log2;
+      s = (p.flip ? -dot : dot) * p.scale_log2;
     }
     float high = s;
 #pragma unroll

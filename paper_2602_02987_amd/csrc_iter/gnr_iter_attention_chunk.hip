@@ -87,16 +87,45 @@ struct Loader {
   {
     if constexpr (kLate) return;
     look_up(p, table, k0, to);
+    if constexpr (!kFp8 && !kSmallPages) {
+      // Addresses in scalar registers but for what does not change: the row within a load's and the piece. A wave issues one instruction
+      // at a time, and this runs beside the products.
+      constexpr int kPeriod = 16 / (kWaves * kRows) > 1 ? 16 / (kWaves * kRows) : 1;   // loads until the order of pieces repeats
+      const int in = key - wave * kRows;
+      uint32_t k_off[kPeriod], v_off[kPeriod];
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      int page, place;
-      locate(p, table, k0, to, i, page, place);
-      if constexpr (kFp8) {
-        load_codes(p, page, place, kr[i], vr[i], ks[i], vs[i]);
-      } else {
-        const int row0 = (i * kWaves + wave) * kRows, from = piece_of<kDim>(row0 + key - wave * kRows, piece) * 16;
-        load_to_lds(keys + page * p.cache.k.page_stride * 2 + place * p.cache.k.place_stride * 2 + from, key_rows + row0 * kRowBytes);
-        load_to_lds(values + page * p.cache.v.page_stride * 2 + place * p.cache.v.place_stride * 2 + from, value_rows + row0 * kRowBytes);
+      for (int i = 0; i < kPeriod; ++i) {
+        const int piece16 = piece_of<kDim>(i * kWaves * kRows + key, piece) * 16;
+        k_off[i] = in * static_cast<uint32_t>(p.cache.k.place_stride * 2) + piece16;
+        v_off[i] = in * static_cast<uint32_t>(p.cache.v.place_stride * 2) + piece16;
+      }
+      const char *k = nullptr, *v = nullptr;
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int row0 = (i * kWaves + wave) * kRows;
+        if (i == 0 || p.page_shift < 6) {
+          const int64_t page = __builtin_amdgcn_readlane(pages_ahead, 4 * next_block + row0 / 16), place = (k0 + row0) & (p.cache.page - 1);
+          k = keys + (page * p.cache.k.page_stride + place * p.cache.k.place_stride) * 2;
+          v = values + (page * p.cache.v.page_stride + place * p.cache.v.place_stride) * 2;
+        } else {
+          k += kWaves * kRows * 2 * p.cache.k.place_stride;
+          v += kWaves * kRows * 2 * p.cache.v.place_stride;
+        }
+        load_to_lds(k + k_off[i % kPeriod], key_rows + row0 * kRowBytes);
+        load_to_lds(v + v_off[i % kPeriod], value_rows + row0 * kRowBytes);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        int page, place;
+        locate(p, table, k0, to, i, page, place);
+        if constexpr (kFp8) {
+          load_codes(p, page, place, kr[i], vr[i], ks[i], vs[i]);
+        } else {
+          const int row0 = (i * kWaves + wave) * kRows, from = piece_of<kDim>(row0 + key - wave * kRows, piece) * 16;
+          load_to_lds(keys + page * p.cache.k.page_stride * 2 + place * p.cache.k.place_stride * 2 + from, key_rows + row0 * kRowBytes);
+          load_to_lds(values + page * p.cache.v.page_stride * 2 + place * p.cache.v.place_stride * 2 + from, value_rows + row0 * kRowBytes);
+        }
       }
     }
     ++next_block;
@@ -192,7 +221,7 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
       const uint16_t *at = static_cast<const uint16_t *>(p.q.data) + static_cast<int64_t>(rq.first + real / p.group) * p.q.token_stride +
                            (head * p.group + real % p.group) * p.q.head_stride + 8 * h;
 #pragma unroll
-      for (int f = 0; f < kFrags; ++f) q[f] = bits<oct>(*reinterpret_cast<const u32x4 *>(at + 16 * f));
+      for (int f = 0; f < kFrags; ++f) q[f] = bits<oct>(*reinterpret_cast<const u32x4 *>(at + 16 * f) ^ p.flip);
     }
     f32x16 acc[kTiles];
 #pragma unroll
@@ -215,10 +244,6 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
           s[kt] = T::mfma32(bits<oct>(a), q[f], s[kt]);
         }
       }
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[kt][i] *= p.scale_log2;
       if (k0 < wave_all_begin || k0 + kKeys > wave_all_end) {
         const int see_from = see_begin - k0, see_to = see_end - k0;
 #pragma unroll
@@ -235,6 +260,7 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
 #pragma unroll
         for (int i = 0; i < 16; ++i) high = fmaxf(high, s[kt][i]);
       // the running maximum moves when a score exceeds it by 2^8: most blocks need no exchange and no rescaling
+      high *= p.scale_log2;
       if (__any(high - top > 8.0f)) {
         high = fmaxf(high, __shfl_xor(high, 32));
         const float next = fmaxf(top, high), keep = __builtin_amdgcn_exp2f(top - next);
@@ -250,7 +276,7 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
       for (int kt = 0; kt < 2; ++kt) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          s[kt][i] = __builtin_amdgcn_exp2f(s[kt][i] - top);
+          s[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], p.scale_log2, -top));
           sum += s[kt][i];
         }
 #pragma unroll
@@ -282,19 +308,21 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
       again = missing_page(p, table, from, to);
       loader.begin(p, head);
       loader.bring(p, table, from, to, keys[0], values[0]);
-      int buffer = 0;
-      for (int k0 = from; k0 < to; k0 += kKeys) {
-        loader.arrive(p, table, k0, to, keys[buffer], values[buffer]);
+      const auto block = [&](int k0, char *key_rows, char *value_rows, char *next_keys, char *next_values) {
+        loader.arrive(p, table, k0, to, key_rows, value_rows);
         __syncthreads();                                        // it is there, and nobody reads the other one any more
         if (k0 + kKeys > min(to, tile_all_end) || k0 < tile_all_begin) {
           // A weight of zero does not silence a NaN or an infinity: where any stands among values that not every row sees, the rows
           // are computed again by the kernel that joins.
-          again |= loader.clear_values(values[buffer], k0, tile_from, to);
+          again |= loader.clear_values(value_rows, k0, tile_from, to);
           __syncthreads();
         }
-        if (k0 + kKeys < to) loader.bring(p, table, k0 + kKeys, to, keys[buffer ^ 1], values[buffer ^ 1]);
-        multiply(k0, keys[buffer], values[buffer]);
-        buffer ^= 1;
+        if (k0 + kKeys < to) loader.bring(p, table, k0 + kKeys, to, next_keys, next_values);
+        multiply(k0, key_rows, value_rows);
+      };
+      for (int k0 = from; k0 < to; k0 += 2 * kKeys) {           // (two at a time: addresses in shared memory are constants)
+        block(k0, keys[0], values[0], keys[1], values[1]);
+        if (k0 + kKeys < to) block(k0 + kKeys, keys[1], values[1], keys[0], values[0]);
       }
     }
     again = __syncthreads_or(again);                            // (and nobody reads the last block any more)

@@ -45,7 +45,7 @@ struct Tile {
 #pragma unroll
     for (int f = 0; f < kFrags; ++f) {
       u32x4 w = {0, 0, 0, 0};
-      if (row) w = *reinterpret_cast<const u32x4 *>(row + element(f));
+      if (row) w = *reinterpret_cast<const u32x4 *>(row + element(f)) ^ p.flip;
       q[f] = bits<oct>(w);
     }
 #pragma unroll
@@ -142,13 +142,14 @@ struct Tile {
 
   // Weights of the 32 keys; the running maximum moves when a score exceeds it by 2^8, so that most blocks need no exchange between
   // lanes and no rescaling (weights stay below 2^8, sums and products lose nothing).
-  __device__ __forceinline__ void weigh(f32x4 *s, uint32_t *w)
+  __device__ __forceinline__ void weigh(f32x4 *s, uint32_t *w, float scale)
   {
     float high = -INFINITY;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) high = fmaxf(high, s[t][i]);
+    high *= scale;
     if (__any(high - top > 8.0f)) {
       high = fmaxf(high, __shfl_xor(high, 16));
       high = fmaxf(high, __shfl_xor(high, 32));
@@ -163,7 +164,7 @@ struct Tile {
     for (int t = 0; t < 2; ++t) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        s[t][i] = __builtin_amdgcn_exp2f(s[t][i] - top);
+        s[t][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], scale, -top));
         sum += s[t][i];
       }
       w[2 * t] = T::narrow2(s[t][0], s[t][1]);
@@ -286,8 +287,6 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : kDim == 128 ? 2 : 
             next_pages(k1);
             rows.load_keys(p, k1, pages, table, stop);
           }
-#pragma unroll
-          for (int t = 0; t < 2; ++t) s[t] *= p.scale_log2;
           if (ragged) {
             const int see_end = min(pos + 1, stop) - k0 - 4 * rows.g, see_begin = (p.window ? pos - p.window + 1 : 0) - k0 - 4 * rows.g;
 #pragma unroll
@@ -299,7 +298,7 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : kDim == 128 ? 2 : 
             again |= rows.clear_values(k0, p.window ? first_pos - p.window + 1 : 0, stop) && first_pos != last_pos;
           }
           uint32_t w[4];
-          rows.weigh(s, w);
+          rows.weigh(s, w, p.scale_log2);
           rows.add_values(w);
           if (!more) break;
           rows.load_values(p, k1, pages, table, stop);

@@ -15,7 +15,8 @@ struct AttentionParams {
   iter_rows q, out;
   int type, heads, group;      // group: query heads to a kv head
   int page_shift;
-  float scale_log2;            // scale / ln 2: weights are powers of two
+  float scale_log2;            // |scale| / ln 2: weights are powers of two
+  uint32_t flip;               // sign bits of two 16-bit elements if the scale is negative
   int window, room;            // room: the most keys a request can have
   float *workspace;
   // of the kernel for few rows (0) and the one for chunks (1): rows of the requests it takes, workgroups, first word of its parts

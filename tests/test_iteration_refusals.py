@@ -62,7 +62,7 @@ def test_the_library_exports_the_header_and_agrees_on_the_structures():
 
 BAD_CACHES = [dict(type=3), dict(type=-1), dict(kv_heads=0), dict(head_dim=96), dict(head_dim=0), dict(page=0), dict(page=24), dict(page=1 << 17),
               dict(pages=-1), dict(pages=1 << 31)]
-BAD_PLANES = [dict(data=None), dict(data=P + 8), dict(page_stride=-8), dict(head_stride=4), dict(place_stride=129), dict(page_stride=1 << 41),
+BAD_PLANES = [dict(data=None), dict(data=P + 8), dict(page_stride=-8), dict(head_stride=4), dict(place_stride=129), dict(page_stride=1 << 41), dict(place_stride=1 << 25),
               dict(exp=P)]
 
 
