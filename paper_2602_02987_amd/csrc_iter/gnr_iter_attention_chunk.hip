@@ -18,41 +18,37 @@ __device__ __forceinline__ int piece_of(int key, int piece)
   else return piece ^ ((key & 3) << 2 | (key >> 2 & 3));
 }
 
-// Brings blocks of keys and values from the cache into shared memory. A wave's load covers kRows neighbouring keys, within a page unless pages are
-// small; 16-bit rows go there directly, 8-bit codes by way of registers, where they are widened.
+// Brings blocks of keys, or of values, from the cache into shared memory. A wave's load covers kRows neighbouring keys, within a page unless
+// pages are small; 16-bit rows go there directly, 8-bit codes by way of registers, where they are widened.
 template <class T, int kDim, bool kFp8, bool kSmallPages>
 struct Loader {
   static constexpr int kPieces = kDim / 8, kRowBytes = kDim * 2;
   static constexpr int kMine = ChunkShape::kKeys * kPieces / kThreads;   // pieces of a block that a thread brings in
-  static constexpr int kRows = 64 / kPieces;                             // keys of a wave's load; kWaves * kRows lie between a thread's
+  static constexpr int kRows = 64 / kPieces, kStep = kWaves * kRows;     // keys of a wave's load, and those between a thread's
   static constexpr int kSize = kFp8 ? 1 : 2;
-  const int wave, key, piece;                                            // this thread's first key of a block, and its place in LDS rows
-  const char *keys, *values;                                             // rows of the kv head
-  const uint8_t *key_exps, *value_exps;
-  u32x2 kr[kFp8 ? kMine : 1], vr[kFp8 ? kMine : 1];
-  uint8_t ks[kFp8 ? kMine : 1], vs[kFp8 ? kMine : 1];
-  int pages_ahead, next_block;                                           // pages of the sixteens of 16 blocks, a lane for each
-
-  __device__ __forceinline__ Loader(int wave_, int lane) : wave(wave_), key(wave_ * kRows + lane / kPieces), piece(lane % kPieces) {}
-
-  __device__ __forceinline__ void begin(const AttentionParams &p, int head)
-  {
-    keys = static_cast<const char *>(p.cache.k.data) + head * p.cache.k.head_stride * kSize;
-    values = static_cast<const char *>(p.cache.v.data) + head * p.cache.v.head_stride * kSize;
-    if constexpr (kFp8) {
-      key_exps = p.cache.k.exp + head * p.cache.k.exp_head_stride;
-      value_exps = p.cache.v.exp + head * p.cache.v.exp_head_stride;
-    }
-    next_block = 16;
-  }
-
   // Rows of 256 elements in 8 bits are loaded when they are due: there are no registers to hold them meanwhile.
   static constexpr bool kLate = kFp8 && kDim == 256;
+  const iter_plane &plane;
+  const int wave, key, piece;                                            // this thread's first key of a block, and its place in LDS rows
+  const char *rows;                                                      // of the kv head
+  const uint8_t *exps;
+  u32x2 codes[kFp8 ? kMine : 1];
+  uint8_t exp[kFp8 ? kMine : 1];
+  int pages_ahead, next_block;                                           // pages of the sixteens of 16 blocks, a lane for each
+
+  __device__ __forceinline__ Loader(const iter_plane &c, int w, int lane) : plane(c), wave(w), key(w * kRows + lane / kPieces), piece(lane % kPieces) {}
+
+  __device__ __forceinline__ void begin(int head)
+  {
+    rows = static_cast<const char *>(plane.data) + head * plane.head_stride * kSize;
+    if constexpr (kFp8) exps = plane.exp + head * plane.exp_head_stride;
+    next_block = 16;
+  }
 
   // A thread's i-th piece of the block at k0: where it lies in the cache. What lies beyond `to` is any row.
   __device__ __forceinline__ void locate(const AttentionParams &p, const int32_t *table, int k0, int to, int i, int &page, int &place) const
   {
-    const int row0 = (i * kWaves + wave) * kRows, in = key - wave * kRows;   // of the block
+    const int row0 = i * kStep + wave * kRows, in = key - wave * kRows;   // of the block
     if constexpr (kSmallPages) {
       const int at = min(k0 + row0 + in, to - 1);
       page = usable_page(p, table[at >> p.page_shift]);
@@ -74,45 +70,36 @@ struct Loader {
     }
   }
 
-  __device__ __forceinline__ void load_codes(const AttentionParams &p, int page, int place, u32x2 &k, u32x2 &v, uint8_t &k_exp, uint8_t &v_exp) const
+  __device__ __forceinline__ void load_codes(int page, int place, int i)
   {
-    k = *reinterpret_cast<const u32x2 *>(keys + page * p.cache.k.page_stride + place * p.cache.k.place_stride + piece * 8);
-    v = *reinterpret_cast<const u32x2 *>(values + page * p.cache.v.page_stride + place * p.cache.v.place_stride + piece * 8);
-    k_exp = key_exps[page * p.cache.k.exp_page_stride + place * p.cache.k.exp_place_stride];
-    v_exp = value_exps[page * p.cache.v.exp_page_stride + place * p.cache.v.exp_place_stride];
+    codes[i] = *reinterpret_cast<const u32x2 *>(rows + page * plane.page_stride + place * plane.place_stride + piece * 8);
+    exp[i] = exps[page * plane.exp_page_stride + place * plane.exp_place_stride];
   }
 
   // Starts on the block of keys from k0 on.
-  __device__ __forceinline__ void bring(const AttentionParams &p, const int32_t *table, int k0, int to, char *key_rows, char *value_rows)
+  __device__ __forceinline__ void bring(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
   {
     if constexpr (kLate) return;
     look_up(p, table, k0, to);
     if constexpr (!kFp8 && !kSmallPages) {
       // Addresses in scalar registers but for what does not change: the row within a load's and the piece. A wave issues one instruction
       // at a time, and this runs beside the products.
-      constexpr int kPeriod = 16 / (kWaves * kRows) > 1 ? 16 / (kWaves * kRows) : 1;   // loads until the order of pieces repeats
-      const int in = key - wave * kRows;
-      uint32_t k_off[kPeriod], v_off[kPeriod];
+      constexpr int kPeriod = 16 / kStep > 1 ? 16 / kStep : 1;           // loads until the order of pieces repeats
+      uint32_t offset[kPeriod];
 #pragma unroll
-      for (int i = 0; i < kPeriod; ++i) {
-        const int piece16 = piece_of<kDim>(i * kWaves * kRows + key, piece) * 16;
-        k_off[i] = in * static_cast<uint32_t>(p.cache.k.place_stride * 2) + piece16;
-        v_off[i] = in * static_cast<uint32_t>(p.cache.v.place_stride * 2) + piece16;
-      }
-      const char *k = nullptr, *v = nullptr;
+      for (int i = 0; i < kPeriod; ++i)
+        offset[i] = (key - wave * kRows) * static_cast<uint32_t>(plane.place_stride * 2) + piece_of<kDim>(i * kStep + key, piece) * 16;
+      const char *from = nullptr;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
-        const int row0 = (i * kWaves + wave) * kRows;
+        const int row0 = i * kStep + wave * kRows;
         if (i == 0 || p.page_shift < 6) {
           const int64_t page = __builtin_amdgcn_readlane(pages_ahead, 4 * next_block + row0 / 16), place = (k0 + row0) & (p.cache.page - 1);
-          k = keys + (page * p.cache.k.page_stride + place * p.cache.k.place_stride) * 2;
-          v = values + (page * p.cache.v.page_stride + place * p.cache.v.place_stride) * 2;
+          from = rows + (page * plane.page_stride + place * plane.place_stride) * 2;
         } else {
-          k += kWaves * kRows * 2 * p.cache.k.place_stride;
-          v += kWaves * kRows * 2 * p.cache.v.place_stride;
+          from += kStep * 2 * plane.place_stride;
         }
-        load_to_lds(k + k_off[i % kPeriod], key_rows + row0 * kRowBytes);
-        load_to_lds(v + v_off[i % kPeriod], value_rows + row0 * kRowBytes);
+        load_to_lds(from + offset[i % kPeriod], lds + row0 * kRowBytes);
       }
     } else {
 #pragma unroll
@@ -120,11 +107,10 @@ struct Loader {
         int page, place;
         locate(p, table, k0, to, i, page, place);
         if constexpr (kFp8) {
-          load_codes(p, page, place, kr[i], vr[i], ks[i], vs[i]);
+          load_codes(page, place, i);
         } else {
-          const int row0 = (i * kWaves + wave) * kRows, from = piece_of<kDim>(row0 + key - wave * kRows, piece) * 16;
-          load_to_lds(keys + page * p.cache.k.page_stride * 2 + place * p.cache.k.place_stride * 2 + from, key_rows + row0 * kRowBytes);
-          load_to_lds(values + page * p.cache.v.page_stride * 2 + place * p.cache.v.place_stride * 2 + from, value_rows + row0 * kRowBytes);
+          const int row0 = i * kStep + wave * kRows;
+          load_to_lds(rows + (page * plane.page_stride + place * plane.place_stride) * 2 + piece_of<kDim>(i * kStep + key, piece) * 16, lds + row0 * kRowBytes);
         }
       }
     }
@@ -132,20 +118,22 @@ struct Loader {
   }
 
   // The block that was started on is there for the workgroup after the next barrier.
-  __device__ __forceinline__ void arrive(const AttentionParams &p, const int32_t *table, int k0, int to, char *key_rows, char *value_rows)
+  __device__ __forceinline__ void arrive(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
   {
     if constexpr (kFp8) {
       if constexpr (kLate) look_up(p, table, k0, to);
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
-        const int row = i * kWaves * kRows + key, at = row * kRowBytes + piece_of<kDim>(row, piece) * 16;
+        const int row = i * kStep + key;
         if constexpr (kLate) {
           int page, place;
           locate(p, table, k0, to, i, page, place);
-          load_codes(p, page, place, kr[i], vr[i], ks[i], vs[i]);
+          load_codes(page, place, i);
         }
-        *reinterpret_cast<u32x4 *>(key_rows + at) = widen(kr[i], exponent_scale(ks[i]));
-        *reinterpret_cast<u32x4 *>(value_rows + at) = widen(vr[i], exponent_scale(vs[i]));
+        const float scale = exponent_scale(exp[i]);
+        *reinterpret_cast<u32x4 *>(lds + row * kRowBytes + piece_of<kDim>(row, piece) * 16) =
+            u32x4{T::template from_e4m3<false>(codes[i][0], scale), T::template from_e4m3<true>(codes[i][0], scale),
+                  T::template from_e4m3<false>(codes[i][1], scale), T::template from_e4m3<true>(codes[i][1], scale)};
       }
       if constexpr (kLate) ++next_block;
     } else {
@@ -153,20 +141,15 @@ struct Loader {
     }
   }
 
-  static __device__ __forceinline__ u32x4 widen(u32x2 x, float scale)
-  {
-    return u32x4{T::template from_e4m3<false>(x[0], scale), T::template from_e4m3<true>(x[0], scale),
-                 T::template from_e4m3<false>(x[1], scale), T::template from_e4m3<true>(x[1], scale)};
-  }
-
-  // Values of the block at k0 that nobody sees (keys outside [from, to)) become zeros. Returns whether any of the others that this thread looks at is no number.
-  __device__ __forceinline__ int clear_values(char *value_rows, int k0, int from, int to) const
+  // Rows of the block at k0 that nobody sees (keys outside [from, to)) become zeros. Returns whether any of the others that this thread looks at
+  // holds no number.
+  __device__ __forceinline__ int clear(char *lds, int k0, int from, int to) const
   {
     bool strange = false;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      const int row = i * kWaves * kRows + key;
-      u32x4 *at = reinterpret_cast<u32x4 *>(value_rows + row * kRowBytes + piece * 16);
+      const int row = i * kStep + key;
+      u32x4 *at = reinterpret_cast<u32x4 *>(lds + row * kRowBytes + piece * 16);
       if (k0 + row < from || k0 + row >= to) {
         *at = u32x4{0, 0, 0, 0};
       } else {
@@ -185,14 +168,14 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
   typedef typename T::oct oct;
   constexpr int kKeys = ChunkShape::kKeys, kRowBytes = kDim * 2, kFrags = kDim / 16, kTiles = kDim / 32;
   extern __shared__ int shared[];
-  __shared__ __attribute__((aligned(16))) char keys[2][kKeys * kRowBytes], values[2][kKeys * kRowBytes];
+  __shared__ __attribute__((aligned(16))) char keys[2 * kKeys * kRowBytes], values[2 * kKeys * kRowBytes];
   const int requests = p.batch.requests, kv_heads = p.cache.kv_heads;
   const Plan plan{shared, shared + requests + 1, shared + 2 * (requests + 1)};
   share_out<ChunkShape>(p, plan, gridDim.x);
   if (blockIdx.x == 0) keep_plan(p, plan, ChunkShape::kPlan);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int n = lane % 32, h = lane / 32;
-  Loader<T, kDim, kFp8, kSmallPages> loader(wave, lane);
+  Loader<T, kDim, kFp8, kSmallPages> key_loader(p.cache.k, wave, lane), value_loader(p.cache.v, wave, lane);
   const int64_t units = static_cast<int64_t>(plan.start[requests]) * kv_heads;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int unit = static_cast<int>(u / kv_heads), head = static_cast<int>(u % kv_heads);
@@ -211,9 +194,9 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
     const int tile_from = begin_of(row0), tile_to = end_of(row0 + ChunkShape::kRows - 1);
     const int tile_begin = tile_from & ~63, blocks = max(0, tile_to - tile_begin + kKeys - 1) / kKeys, each = (blocks + splits - 1) / splits;
     const int from = tile_begin + min(blocks, split * each) * kKeys, to = min(tile_to, tile_begin + min(blocks, (split + 1) * each) * kKeys);
-    // what all rows of the tile see, of this wave's, and what any of this wave's sees
+    // what all rows of the tile see, and all of this wave's
     const int tile_all_begin = begin_of(row0 + ChunkShape::kRows - 1), tile_all_end = end_of(row0);
-    const int wave_all_begin = begin_of(wave_row + 31), wave_all_end = end_of(wave_row), wave_begin = begin_of(wave_row), wave_end = end_of(wave_row + 31);
+    const int wave_all_begin = begin_of(wave_row + 31), wave_all_end = end_of(wave_row);
     const int see_begin = begin_of(row) - 4 * h, see_end = end_of(row) - 4 * h;
     oct q[kFrags];
     {
@@ -230,100 +213,133 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
       for (int i = 0; i < 16; ++i) acc[e][i] = 0.0f;
     float top = -FLT_MAX, sum = 0.0f;
 
-    const auto multiply = [&](int k0, const char *key_rows, const char *value_rows) {
-      if (k0 >= wave_end || k0 + kKeys <= wave_begin) return;
-      f32x16 s[2];
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[kt][i] = 0.0f;
-#pragma unroll
-        for (int f = 0; f < kFrags; ++f) {
-          const int key = 32 * kt + n;
-          const u32x4 a = *reinterpret_cast<const u32x4 *>(key_rows + key * kRowBytes + piece_of<kDim>(key, 2 * f + h) * 16);
-          s[kt] = T::mfma32(bits<oct>(a), q[f], s[kt]);
-        }
-      }
+    // Operands from shared memory, asked for kAhead products before they are due. What a product and the work beside it need stays together
+    // (sched_barrier): left to itself the compiler reads far ahead and runs out of registers.
+    constexpr int kAhead = 4, kScoreProducts = 2 * kFrags, kValueProducts = 4 * kTiles, kBuffer = kKeys * kRowBytes;
+    // The order of pieces is an exclusive or, so the places of a lane's pieces are one number and constants; another bit says which of two
+    // buffers. The numbers are made anew for every block (by an empty asm): kept, the places of all pieces would fill thirty registers.
+    int key_at = n * kRowBytes + piece_of<kDim>(n, h) * 16, value_at;
+    {
+      const int group = lane / 16, key = 4 * (group / 2) + lane % 16 / 4;
+      value_at = key * kRowBytes + piece_of<kDim>(key, 2 * (group % 2) + lane % 4 / 2) * 16 + lane % 2 * 8;
+    }
+    const auto key_operand = [&](auto i) GNR_INLINE {           // of the i-th product: keys 32 (i % 2) on, elements 16 (i / 2) on
+      return *reinterpret_cast<const u32x4 *>(keys + (key_at ^ 32 * (i / 2)) + 32 * (i % 2) * kRowBytes);
+    };
+    const auto value_operand = [&](auto i) GNR_INLINE {         // of the i-th product: keys 16 (i / kTiles) on, elements 32 (i % kTiles) on
+      const s16x4 a = read_transposed(values + (value_at ^ 64 * (i % kTiles)) + 16 * (i / kTiles) * kRowBytes);
+      const s16x4 b = read_transposed(values + (value_at ^ (64 * (i % kTiles) + 32)) + (16 * (i / kTiles) + 8) * kRowBytes);
+      return bits<u32x4>(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    f32x16 low, high;                                           // scores of this lane's row: keys 8 (i / 4) + 4 h + i % 4 of a block's halves
+    u32x4 w[4];                                                 // weights of a block
+    const auto score = [&]() GNR_INLINE {
+      u32x4 operand[kAhead];
+      repeat<kAhead>([&](auto i) GNR_INLINE { operand[i] = key_operand(i); });
+      low = high = f32x16{0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+      repeat<kScoreProducts>([&](auto i) GNR_INLINE {
+        f32x16 &x = i % 2 ? high : low;
+        x = T::mfma32(bits<oct>(operand[i % kAhead]), q[i / 2], x);
+        if constexpr (i + kAhead < kScoreProducts) operand[i % kAhead] = key_operand(std::integral_constant<int, i + kAhead>{});
+        __builtin_amdgcn_sched_barrier(0);
+      });
+    };
+    // Hides what the row does not see. The running maximum moves when a score exceeds it by 2^8: most blocks need no exchange and no
+    // rescaling. Returns what to scale the sums before by (1: nothing moved, in the whole wave).
+    const auto settle = [&](int k0) GNR_INLINE {
       if (k0 < wave_all_begin || k0 + kKeys > wave_all_end) {
         const int see_from = see_begin - k0, see_to = see_end - k0;
-#pragma unroll
-        for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int key = 32 * kt + 8 * (i / 4) + i % 4;      // (4 h is in the bounds)
-            s[kt][i] = key >= see_from && key < see_to ? s[kt][i] : -INFINITY;
-          }
+        repeat<16>([&](auto i) GNR_INLINE {
+          constexpr int at = i, key = 8 * (i / 4) + i % 4;      // (4 h is in the bounds)
+          low[at] = key >= see_from && key < see_to ? low[at] : -INFINITY;
+          high[at] = key + 32 >= see_from && key + 32 < see_to ? high[at] : -INFINITY;
+        });
       }
-      float high = -INFINITY;
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) high = fmaxf(high, s[kt][i]);
-      // the running maximum moves when a score exceeds it by 2^8: most blocks need no exchange and no rescaling
-      high *= p.scale_log2;
-      if (__any(high - top > 8.0f)) {
-        high = fmaxf(high, __shfl_xor(high, 32));
-        const float next = fmaxf(top, high), keep = __builtin_amdgcn_exp2f(top - next);
+      float most = -INFINITY;
+      repeat<16>([&](auto i) GNR_INLINE {
+        constexpr int at = i;
+        most = fmaxf(fmaxf(most, low[at]), high[at]);
+      });
+      most *= p.scale_log2;
+      float keep = 1.0f;
+      if (__any(most - top > 8.0f)) {
+        most = fmaxf(most, __shfl_xor(most, 32));
+        const float next = fmaxf(top, most);
+        keep = __builtin_amdgcn_exp2f(top - next);
         top = next;
         sum *= keep;
-#pragma unroll
-        for (int e = 0; e < kTiles; ++e)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[e][i] *= keep;
       }
-      oct w[4];
-#pragma unroll
-      for (int kt = 0; kt < 2; ++kt) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[kt][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[kt][i], p.scale_log2, -top));
-          sum += s[kt][i];
-        }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          u32x4 x;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) x[k] = T::narrow2(s[kt][8 * half + 2 * k], s[kt][8 * half + 2 * k + 1]);
-          w[2 * kt + half] = bits<oct>(x);
-        }
-      }
-      const int group = lane / 16, from_key = 4 * (group / 2) + lane % 16 / 4, from_piece = 2 * (group % 2) + lane % 4 / 2;
-#pragma unroll
-      for (int e = 0; e < kTiles; ++e)
-#pragma unroll
-        for (int kb = 0; kb < 4; ++kb) {
-          s16x4 part[2];
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) {
-            const int key = 16 * kb + 8 * jj + from_key;
-            part[jj] = read_transposed(value_rows + key * kRowBytes + piece_of<kDim>(key, 4 * e + from_piece) * 16 + lane % 2 * 8);
-          }
-          const s16x8 a = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-          acc[e] = T::mfma32(bits<oct>(a), w[kb], acc[e]);
-        }
+      return keep;
+    };
+    const auto weigh = [&](u32x4 (&to_weights)[4], auto i) GNR_INLINE {   // scores 2 i and 2 i + 1
+      constexpr int j = 2 * (i % 8), word = i % 4;
+      const f32x16 &x = i < 8 ? low : high;
+      const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], p.scale_log2, -top)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], p.scale_log2, -top));
+      sum += a;
+      sum += b;
+      to_weights[i / 4][word] = T::narrow2(a, b);
+    };
+    // The weights' products with their values and, beside them, the weights of the block after, whose scores are there already.
+    const auto add = [&](auto also, u32x4 (&next)[4]) GNR_INLINE {
+      constexpr int kEach = kValueProducts < 16 ? 16 / kValueProducts : 1;
+      u32x4 operand[kAhead];
+      repeat<kAhead>([&](auto i) GNR_INLINE { operand[i] = value_operand(i); });
+      repeat<kValueProducts>([&](auto i) GNR_INLINE {
+        acc[i % kTiles] = T::mfma32(bits<oct>(operand[i % kAhead]), bits<oct>(w[i / kTiles]), acc[i % kTiles]);
+        if constexpr (i + kAhead < kValueProducts) operand[i % kAhead] = value_operand(std::integral_constant<int, i + kAhead>{});
+        if constexpr (also && (kValueProducts <= 16 || i % 2 == 0))
+          repeat<kEach>([&](auto k) GNR_INLINE { weigh(next, std::integral_constant<int, 16 * i / kValueProducts + k>{}); });
+        __builtin_amdgcn_sched_barrier(0);
+      });
     };
 
     int again = 0;
     if (from < to) {
       again = missing_page(p, table, from, to);
-      loader.begin(p, head);
-      loader.bring(p, table, from, to, keys[0], values[0]);
-      const auto block = [&](int k0, char *key_rows, char *value_rows, char *next_keys, char *next_values) {
-        loader.arrive(p, table, k0, to, key_rows, value_rows);
-        __syncthreads();                                        // it is there, and nobody reads the other one any more
+      key_loader.begin(head);
+      value_loader.begin(head);
+      int buffer = 0;                                           // kBuffer for the second one; of the block whose values are due
+      key_loader.bring(p, table, from, to, keys);
+      key_loader.arrive(p, table, from, to, keys);
+      __syncthreads();
+      value_loader.bring(p, table, from, to, values);
+      if (from + kKeys < to) key_loader.bring(p, table, from + kKeys, to, keys + kBuffer);
+      score();
+      settle(from);
+      repeat<16>([&](auto i) GNR_INLINE { weigh(w, i); });
+      // A weight of zero does not silence a NaN or an infinity: where any stands among values that not every row sees, the rows are
+      // computed again by the kernel that joins.
+      const auto check_values = [&](int k0) GNR_INLINE {
         if (k0 + kKeys > min(to, tile_all_end) || k0 < tile_all_begin) {
-          // A weight of zero does not silence a NaN or an infinity: where any stands among values that not every row sees, the rows
-          // are computed again by the kernel that joins.
-          again |= loader.clear_values(value_rows, k0, tile_from, to);
+          again |= value_loader.clear(values + buffer, k0, tile_from, to);
           __syncthreads();
         }
-        if (k0 + kKeys < to) loader.bring(p, table, k0 + kKeys, to, next_keys, next_values);
-        multiply(k0, key_rows, value_rows);
       };
-      for (int k0 = from; k0 < to; k0 += 2 * kKeys) {           // (two at a time: addresses in shared memory are constants)
-        block(k0, keys[0], values[0], keys[1], values[1]);
-        if (k0 + kKeys < to) block(k0 + kKeys, keys[1], values[1], keys[0], values[0]);
+      // Keys come in a block ahead of values: the scores of the block after are there when a block's weights meet their values, so that the
+      // exponentials run beside these products.
+      int k0 = from;
+      for (; k0 + kKeys < to; k0 += kKeys) {
+        asm volatile("" : "+v"(key_at), "+v"(value_at));
+        key_at ^= kBuffer;
+        value_loader.arrive(p, table, k0, to, values + buffer);
+        key_loader.arrive(p, table, k0 + kKeys, to, keys + (buffer ^ kBuffer));
+        __syncthreads();                                        // they are there, and nobody reads the ones before any more
+        check_values(k0);
+        value_loader.bring(p, table, k0 + kKeys, to, values + (buffer ^ kBuffer));
+        if (k0 + 2 * kKeys < to) key_loader.bring(p, table, k0 + 2 * kKeys, to, keys + buffer);
+        score();
+        const float keep = settle(k0 + kKeys);
+        u32x4 next[4];
+        add(std::true_type{}, next);
+        if (__any(keep != 1.0f)) repeat<kTiles>([&](auto e) GNR_INLINE { acc[e] *= keep; });
+        repeat<4>([&](auto i) GNR_INLINE { w[i] = next[i]; });
+        value_at ^= kBuffer;
+        buffer ^= kBuffer;
       }
+      value_loader.arrive(p, table, k0, to, values + buffer);
+      __syncthreads();
+      check_values(k0);
+      add(std::false_type{}, w);
     }
     again = __syncthreads_or(again);                            // (and nobody reads the last block any more)
     if (threadIdx.x == 0) mark_unit(p, ChunkShape::kPlan, u, again);

@@ -62,6 +62,17 @@ struct Fp16 {
 
 __device__ __forceinline__ float exponent_scale(uint32_t byte) { return bits<float>(byte << 23); }
 
+// f(0) .. f(kN - 1) with numbers that are constants: arrays that are indexed by them stay in registers.
+template <int kN, int kAt = 0, class F>
+__device__ __forceinline__ void repeat(const F &f)
+{
+  if constexpr (kAt < kN) {
+    f(std::integral_constant<int, kAt>{});
+    repeat<kN, kAt + 1>(f);
+  }
+}
+#define GNR_INLINE __attribute__((always_inline))
+
 // Whether either of two 16-bit values is a NaN or an infinity.
 template <class T>
 __device__ __forceinline__ bool no_number(uint32_t w) { return (w & T::kInf) == T::kInf || (w >> 16 & T::kInf) == T::kInf; }
