@@ -177,7 +177,12 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
   const int n = lane % 32, h = lane / 32;
   Loader<T, kDim, kFp8, kSmallPages> key_loader(p.cache.k, wave, lane), value_loader(p.cache.v, wave, lane);
   const int64_t units = static_cast<int64_t>(plan.start[requests]) * kv_heads;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+  // Units are dealt out heaviest first and back and forth, so that every workgroup has as much to do; a head stays with the workgroups of
+  // one place among eight, which share a cache.
+  const int dealt = gridDim.x % kv_heads == 0 ? kv_heads : 1, back = gridDim.x / dealt - 1 - blockIdx.x / dealt;
+  for (int64_t round = 0; round * gridDim.x < units; ++round) {
+    const int64_t u = round * gridDim.x + (round % 2 ? back * dealt + blockIdx.x % dealt : blockIdx.x);
+    if (u >= units) continue;
     const int unit = static_cast<int>(u / kv_heads), head = static_cast<int>(u % kv_heads);
     const int r = __builtin_amdgcn_readfirstlane(last_not_above(plan.start, requests, unit));
     uint32_t flags = 0;
@@ -277,7 +282,9 @@ __global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_c
       const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], p.scale_log2, -top)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], p.scale_log2, -top));
       sum += a;
       sum += b;
-      to_weights[i / 4][word] = T::narrow2(a, b);
+      uint32_t both = T::narrow2(a, b);
+      asm volatile("" : "+v"(both));                            // (stays where it is: the compiler would move it all behind the products)
+      to_weights[i / 4][word] = both;
     };
     // The weights' products with their values and, beside them, the weights of the block after, whose scores are there already.
     const auto add = [&](auto also, u32x4 (&next)[4]) GNR_INLINE {
