@@ -39,7 +39,7 @@ enum iter_type { ITER_BF16 = 0, ITER_FP16 = 1, ITER_FP8 = 2 };
 enum iter_status { ITER_BAD_BATCH = 1, ITER_BAD_PAGE = 2, ITER_BAD_ADAPTER = 4 };
 
 /* Keys or values of a paged cache: element (page, head, place, d) is data[page*page_stride + head*head_stride +
- * place*place_stride + d], strides in elements, non-negative (place_stride at most 2^24), the data and every row 16-byte aligned. Of an FP8 cache the row (page, head,
+ * place*place_stride + d], strides in elements, non-negative (place_stride and exp_place_stride at most 2^24), the data and every row 16-byte aligned. Of an FP8 cache the row (page, head,
  * place) stands for its codes times 2^(exp - 127), where exp is the byte at exp[page*exp_page_stride + head*exp_head_stride +
  * place*exp_place_stride] (1..254); other caches have no exponents (NULL). */
 typedef struct {

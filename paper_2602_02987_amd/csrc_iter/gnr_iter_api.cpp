@@ -34,7 +34,7 @@ bool plane_ok(const iter_cache &c, const iter_plane &p)
   if (c.type != ITER_FP8) return p.exp == nullptr;
   for (const int64_t s : {p.exp_page_stride, p.exp_head_stride, p.exp_place_stride})
     if (s < 0 || s > kMaxStride) return false;
-  return span_ok(c.pages, p.exp_page_stride) && (c.pages == 0 || p.exp != nullptr);
+  return p.exp_place_stride <= kMaxPlaceStride && span_ok(c.pages, p.exp_page_stride) && (c.pages == 0 || p.exp != nullptr);
 }
 
 bool cache_ok(const iter_cache *c)

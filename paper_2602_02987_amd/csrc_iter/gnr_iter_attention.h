@@ -14,8 +14,12 @@ constexpr int kPartTail = 4;                   // words of a part after its sums
 
 // A kernel takes the requests with `least` to `most` rows (tokens times query heads of a kv head), in tiles of kRows rows and blocks
 // of kKeys keys, about kPieces pieces to a workgroup.
-struct RowsShape { static constexpr int kRows = 16, kKeys = 32 * kWaves, kPieces = 4, kBlocks = 512, kPlan = 0; };
-struct ChunkShape { static constexpr int kRows = 128, kKeys = 64, kPieces = 1, kBlocks = 512, kPlan = 1; };
+struct RowsShape { static constexpr int kRows = 16, kKeys = 32 * kWaves, kPieces = 4, kPlan = 0; };
+struct ChunkShape { static constexpr int kRows = 128, kKeys = 64, kPieces = 1, kPlan = 1; };
+// Workgroups that a compute unit holds at once, by their registers.
+constexpr int kComputeUnits = 256;
+constexpr int rows_blocks(int dim, bool fp8) { return dim == 256 ? 1 : dim == 128 && !fp8 ? 2 : 3; }
+constexpr int chunk_blocks(int dim) { return dim == 256 ? 1 : 2; }
 constexpr int kFewRows = 16;
 
 // What a request asks for. Bounds that contradict each other or the arrays are cut down to what is inside them. Positions are below 2^30.

@@ -186,8 +186,8 @@ static int64_t decide(AttentionParams &p)
     const int64_t units = (p.batch.requests + rows / tile) * ((keys + block - 1) / block + 1) * p.cache.kv_heads;
     return !used ? 0 : units < most ? units : most;
   };
-  p.blocks[0] = static_cast<int>(blocks(few, RowsShape::kBlocks, RowsShape::kRows, RowsShape::kKeys));
-  p.blocks[1] = static_cast<int>(blocks(chunks, ChunkShape::kBlocks, ChunkShape::kRows, ChunkShape::kKeys));
+  p.blocks[0] = static_cast<int>(blocks(few, kComputeUnits * rows_blocks(p.cache.head_dim, p.cache.type == ITER_FP8), RowsShape::kRows, RowsShape::kKeys));
+  p.blocks[1] = static_cast<int>(blocks(chunks, kComputeUnits * chunk_blocks(p.cache.head_dim), ChunkShape::kRows, ChunkShape::kKeys));
   // Units: what the pieces fill, and one more for each tile. A request that is shared out has fewer than twice as many pieces as
   // its keys fill, and only those leave parts.
   const int64_t words = p.cache.head_dim + kPartTail;

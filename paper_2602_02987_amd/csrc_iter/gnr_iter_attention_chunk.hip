@@ -163,7 +163,7 @@ struct Loader {
 };
 
 template <class T, int kDim, bool kFp8, bool kSmallPages>
-__global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : 2) gnr_attention_chunk_kernel(const AttentionParams p)
+__global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_chunk_kernel(const AttentionParams p)
 {
   typedef typename T::oct oct;
   constexpr int kKeys = ChunkShape::kKeys, kRowBytes = kDim * 2, kFrags = kDim / 16, kTiles = kDim / 32;

@@ -38,6 +38,7 @@ struct Tile {
   {
     keys = static_cast<const char *>(p.cache.k.data) + head * p.cache.k.head_stride * kSize;
     values = static_cast<const char *>(p.cache.v.data) + head * p.cache.v.head_stride * kSize;
+    key_exps = value_exps = nullptr;
     if constexpr (kFp8) {
       key_exps = p.cache.k.exp + head * p.cache.k.exp_head_stride;
       value_exps = p.cache.v.exp + head * p.cache.v.exp_head_stride;
@@ -76,41 +77,50 @@ struct Tile {
   __device__ __forceinline__ void load_keys(const AttentionParams &p, int k0, const int *pages, const int32_t *table, int stop)
   {
     const iter_plane &c = p.cache.k;
+    if constexpr (kSmallPages) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      int page, place;
-      if constexpr (kSmallPages) {
-        const int key = min(k0 + 16 * t + n, stop - 1);
-        page = usable_page(p, table[key >> p.page_shift]);
-        place = key & (p.cache.page - 1);
-      } else {
-        page = pages[t];
-        place = ((k0 + 16 * t) & (p.cache.page - 1)) + n;
+      for (int t = 0; t < 2; ++t) {
+        const int key = min(k0 + 16 * t + n, stop - 1), place = key & (p.cache.page - 1);
+        const int64_t page = usable_page(p, table[key >> p.page_shift]);
+        load_key(t, keys + (page * c.page_stride + place * c.place_stride) * kSize + 16 * g, key_exps + (kFp8 ? page * c.exp_page_stride + place * c.exp_place_stride : 0));
       }
-      const char *row = keys + page * c.page_stride * kSize + place * c.place_stride * kSize + 16 * g;
+    } else {
+      // (a wave's address in scalar registers and a lane's offset of 32 bits, which is always the same)
+      const uint32_t lane_row = n * static_cast<uint32_t>(c.place_stride * kSize) + 16 * g, lane_exp = n * static_cast<uint32_t>(c.exp_place_stride);
 #pragma unroll
-      for (int i = 0; i < kKeyWords / 4; ++i) load_words<4>(row + 64 * i, &kw[t][4 * i]);
-      if constexpr (kFp8) ks[t] = key_exps[page * c.exp_page_stride + place * c.exp_place_stride];
+      for (int t = 0; t < 2; ++t) {
+        const int64_t page = pages[t], place = (k0 + 16 * t) & (p.cache.page - 1);
+        load_key(t, keys + (page * c.page_stride + place * c.place_stride) * kSize + lane_row, key_exps + (kFp8 ? page * c.exp_page_stride + place * c.exp_place_stride + lane_exp : 0));
+      }
     }
+  }
+
+  __device__ __forceinline__ void load_key(int t, const char *row, const uint8_t *exp)
+  {
+#pragma unroll
+    for (int i = 0; i < kKeyWords / 4; ++i) load_words<4>(row + 64 * i, &kw[t][4 * i]);
+    if constexpr (kFp8) ks[t] = *exp;
   }
 
   __device__ __forceinline__ void load_values(const AttentionParams &p, int k0, const int *pages, const int32_t *table, int stop)
   {
     const iter_plane &c = p.cache.v;
+    if constexpr (kSmallPages) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int t = j / 4, in = 4 * g + j % 4;
-      int page, place;
-      if constexpr (kSmallPages) {
-        const int key = min(k0 + 16 * t + in, stop - 1);
-        page = usable_page(p, table[key >> p.page_shift]);
-        place = key & (p.cache.page - 1);
-      } else {
-        page = pages[t];
-        place = ((k0 + 16 * t) & (p.cache.page - 1)) + in;
+      for (int j = 0; j < 8; ++j) {
+        const int key = min(k0 + 16 * (j / 4) + 4 * g + j % 4, stop - 1), place = key & (p.cache.page - 1);
+        const int64_t page = usable_page(p, table[key >> p.page_shift]);
+        load_words<kValWords>(values + (page * c.page_stride + place * c.place_stride) * kSize + kVec * kSize * n, vw[j]);
+        if constexpr (kFp8) vs[j] = value_exps[page * c.exp_page_stride + place * c.exp_place_stride];
       }
-      load_words<kValWords>(values + page * c.page_stride * kSize + place * c.place_stride * kSize + kVec * kSize * n, vw[j]);
-      if constexpr (kFp8) vs[j] = value_exps[page * c.exp_page_stride + place * c.exp_place_stride];
+    } else {
+      const uint32_t lane_row = 4 * g * static_cast<uint32_t>(c.place_stride * kSize) + kVec * kSize * n, lane_exp = 4 * g * static_cast<uint32_t>(c.exp_place_stride);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int64_t page = pages[j / 4], place = ((k0 + 16 * (j / 4)) & (p.cache.page - 1)) + j % 4;
+        load_words<kValWords>(values + (page * c.page_stride + place * c.place_stride) * kSize + lane_row, vw[j]);
+        if constexpr (kFp8) vs[j] = (value_exps + (page * c.exp_page_stride + place * c.exp_place_stride))[lane_exp];
+      }
     }
   }
 
@@ -222,7 +232,7 @@ struct Tile {
 };
 
 template <class T, int kDim, bool kFp8, bool kSmallPages>
-__global__ void __launch_bounds__(kThreads, kDim == 256 ? 1 : kDim == 128 ? 2 : 3) gnr_attention_rows_kernel(const AttentionParams p)
+__global__ void __launch_bounds__(kThreads, rows_blocks(kDim, kFp8)) gnr_attention_rows_kernel(const AttentionParams p)
 {
   typedef Tile<T, kDim, kFp8, kSmallPages> Rows;
   extern __shared__ int shared[];

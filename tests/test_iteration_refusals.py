@@ -83,7 +83,7 @@ def test_planes_that_are_refused(bad):
 
 def test_exponents_go_with_8_bits():
     assert _write(_plane(_cache(2), exp=None)) == EINVAL
-    assert _write(_plane(_cache(2), exp_place_stride=-1)) == EINVAL
+    assert _write(_plane(_cache(2), exp_place_stride=-1)) == EINVAL and _write(_plane(_cache(2), exp_place_stride=1 << 25)) == EINVAL
     assert _write(_plane(_cache(2), place_stride=136)) == EINVAL    # rows of 8 bits are aligned to 16 bytes as well
 
 
