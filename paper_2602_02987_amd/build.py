@@ -43,8 +43,6 @@ FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950", "-fPIC", "-ffp-contract=o
          "-mllvm", "-disable-lsr", "-mllvm", "-disable-machine-licm"]
 # the rest of the flags are about the step kernel's registers and atomics
 ITER_FLAGS = FLAGS[:FLAGS.index("-Wno-unused-function") + 1]
-# hoisting what is constant in a loop costs the kernel for few rows more registers than three waves a SIMD have
-SOURCE_FLAGS = {"gnr_iter_attention_rows.hip": ["-mllvm", "-disable-machine-licm"]}
 
 
 def _compile(src: str, force: bool, verbose: bool) -> str:
@@ -55,7 +53,7 @@ def _compile(src: str, force: bool, verbose: bool) -> str:
     deps = [path] + (ITER_HEADERS if iteration else HEADERS)
     if not force and os.path.exists(obj) and all(os.path.getmtime(obj) > os.path.getmtime(d) for d in deps):
         return obj
-    cmd = [HIPCC] + (ITER_FLAGS if iteration else FLAGS) + SOURCE_FLAGS.get(src, []) + [f"-I{INCLUDE}", f"-I{csrc}", "-c", path, "-o", obj]
+    cmd = [HIPCC] + (ITER_FLAGS if iteration else FLAGS) + [f"-I{INCLUDE}", f"-I{csrc}", "-c", path, "-o", obj]
     if verbose:
         print(" ".join(cmd), flush=True)
     r = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)

@@ -13,12 +13,12 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kPartTail = 4;                   // words of a part after its sums: maximum, sum of weights, two of padding
 
 // A kernel takes the requests with `least` to `most` rows (tokens times query heads of a kv head), in tiles of kRows rows and blocks
-// of kKeys keys, about kPieces pieces to a workgroup.
-struct RowsShape { static constexpr int kRows = 16, kKeys = 32 * kWaves, kPieces = 4, kPlan = 0; };
-struct ChunkShape { static constexpr int kRows = 128, kKeys = 64, kPieces = 1, kPlan = 1; };
+// of kKeys keys.
+struct RowsShape { static constexpr int kRows = 16, kKeys = 32 * kWaves, kPlan = 0; };
+struct ChunkShape { static constexpr int kRows = 128, kKeys = 64, kPlan = 1; };
 // Workgroups that a compute unit holds at once, by their registers.
 constexpr int kComputeUnits = 256;
-constexpr int rows_blocks(int dim, bool fp8) { return dim == 256 ? 1 : dim == 128 && !fp8 ? 2 : 3; }
+constexpr int rows_blocks(int dim) { return dim == 256 ? 1 : dim == 128 ? 2 : 3; }
 constexpr int chunk_blocks(int dim) { return dim == 256 ? 1 : 2; }
 constexpr int kFewRows = 16;
 
@@ -48,20 +48,15 @@ __device__ __forceinline__ Request request_of(const AttentionParams &p, int r, u
   return q;
 }
 
-// The plan of a launch, found by every workgroup for itself: before request r lie start[r] units (a piece of the keys of a tile of
-// rows), part[r] rows of parts and join[r] rows that are joined from them.
-struct Plan {
-  int *start, *part, *join;
-};
-
-// Sum of a value over the workgroup and of those of the threads before this one.
-__device__ __forceinline__ void block_scan(int v, int *scratch, int &before, int &total)
+// Sum of a value over the workgroup's threads before this one, and over all.
+template <class V>
+__device__ __forceinline__ void block_scan(V v, V *scratch, V &before, V &total)
 {
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  int x = v;
+  V x = v;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int o = __shfl_up(x, d);
+    const V o = __shfl_up(x, d);
     if (lane >= d) x += o;
   }
   __syncthreads();
@@ -75,53 +70,93 @@ __device__ __forceinline__ void block_scan(int v, int *scratch, int &before, int
   }
 }
 
-__device__ __forceinline__ int64_t block_sum(int64_t v, unsigned long long *scratch)
+// A request's tiles of rows (none, if the kernel does not take it) and the blocks of keys that they see, at least one.
+template <class Shape>
+__device__ __forceinline__ int tiles_of(const AttentionParams &p, const Request &q, int &rows, int &keys)
 {
-#pragma unroll
-  for (int d = 32; d; d /= 2) v += __shfl_xor(v, d);
-  __syncthreads();
-  if (threadIdx.x % 64 == 0) scratch[threadIdx.x / 64] = static_cast<unsigned long long>(v);
-  __syncthreads();
-  int64_t all = 0;
-  for (int w = 0; w < kWaves; ++w) all += static_cast<int64_t>(scratch[w]);
-  return all;
+  rows = q.tokens * p.group;
+  keys = max(1, (q.end - q.begin + Shape::kKeys - 1) / Shape::kKeys);
+  const bool mine = q.tokens > 0 && rows >= p.least[Shape::kPlan] && rows <= p.most[Shape::kPlan];
+  return mine ? (rows + Shape::kRows - 1) / Shape::kRows : 0;
 }
 
-// The keys of a request are shared out in pieces, so that few long rows fill the chip and a long request does not outlast the others: whole
-// blocks of keys, the pieces of a request as long as each other, no more of them in all than fill the workgroups evenly. It is a
-// function of the batch alone, so the same rows are summed in the same order every time, and costs a launch two microseconds, which
-// spares the host from knowing the lengths.
-template <class Shape>
-__device__ __forceinline__ void share_out(const AttentionParams &p, const Plan &plan, int blocks)
+// How a launch shares out its work, found by every workgroup for itself: it is a function of the batch alone, so the same rows are summed in the
+// same order every time, and costs a launch two microseconds, which spares the host from knowing the lengths.
+//
+// Few rows: all blocks of keys of all (tile, kv head) in a row, cut into as many pieces of the same length as there are workgroups: every one reads as
+// much of the cache, however long the requests are. A (tile, kv head) that is cut leaves parts, two at most to a workgroup: one that began
+// before it (slot 0) and one that ends after it or is cut at its very beginning (slot 1).
+struct RowsPlan {
+  int64_t *start;           // blocks of keys before request r, for one kv head
+  int *tiles;               // tiles before request r
+  int64_t total;            // blocks of keys, all heads
+  int blocks;               // workgroups that have any
+  __device__ __forceinline__ int64_t cut(int64_t b) const { return b * total / blocks; }
+  __device__ __forceinline__ int block_of(int64_t x) const { return static_cast<int>(((x + 1) * blocks + total - 1) / total - 1); }
+};
+
+__device__ __forceinline__ RowsPlan share_out_rows(const AttentionParams &p, void *memory, int blocks)
+{
+  __shared__ int64_t scratch64[kWaves];
+  __shared__ int scratch[kWaves];
+  const int n = p.batch.requests;
+  RowsPlan plan{static_cast<int64_t *>(memory), reinterpret_cast<int *>(static_cast<int64_t *>(memory) + n + 1), 0, 0};
+  uint32_t flags = 0;
+  int64_t done64 = 0;
+  int done = 0;
+  for (int r0 = 0; r0 < n; r0 += kThreads) {
+    const int r = r0 + threadIdx.x;
+    int rows = 0, keys = 0, tiles = 0;
+    if (r < n) tiles = tiles_of<RowsShape>(p, request_of(p, r, &flags), rows, keys);
+    int64_t before64, total64;
+    int before, total;
+    block_scan<int64_t>(static_cast<int64_t>(tiles) * keys, scratch64, before64, total64);
+    block_scan<int>(tiles, scratch, before, total);
+    if (r < n) {
+      plan.start[r] = done64 + before64;
+      plan.tiles[r] = done + before;
+    }
+    done64 += total64;
+    done += total;
+  }
+  if (threadIdx.x == 0) {
+    plan.start[n] = done64;
+    plan.tiles[n] = done;
+  }
+  if (flags && p.status && blockIdx.x == 0) atomicOr(p.status, flags);
+  plan.total = uniform(done64) * p.cache.kv_heads;
+  plan.blocks = static_cast<int>(min(plan.total, static_cast<int64_t>(blocks)));
+  __syncthreads();
+  return plan;
+}
+
+// Chunks: a tile of rows is whole where there are many. Where there are few, their keys are cut into pieces, as long as each other within a
+// request, no more of them in all than there are workgroups. Before request r lie start[r] units (a piece of a tile's keys), part[r] rows of parts
+// and join[r] rows that are joined from them.
+struct ChunkPlan {
+  int *start, *part, *join;
+};
+
+__device__ __forceinline__ void share_out_chunks(const AttentionParams &p, const ChunkPlan &plan, int blocks)
 {
   __shared__ int scratch[kWaves];
-  __shared__ unsigned long long sums[kWaves];
+  __shared__ int64_t sums[kWaves];
   const int n = p.batch.requests;
   uint32_t flags = 0;
-  const auto work = [&](int r, int &tiles, int &keys, int &rows) {
-    const Request q = request_of(p, r, &flags);
-    rows = q.tokens * p.group;
-    const bool mine = q.tokens > 0 && rows >= p.least[Shape::kPlan] && rows <= p.most[Shape::kPlan];
-    tiles = mine ? (rows + Shape::kRows - 1) / Shape::kRows : 0;
-    keys = (q.end - q.begin + Shape::kKeys - 1) / Shape::kKeys;
-  };
-  int64_t all = 0;
-  int tiles, keys, rows;
-  for (int r = threadIdx.x; r < n; r += kThreads) {
-    work(r, tiles, keys, rows);
-    all += static_cast<int64_t>(tiles) * keys;
-  }
-  all = block_sum(all, sums) * p.cache.kv_heads;
+  int64_t all = 0, before64;
+  int rows, keys;
+  for (int r = threadIdx.x; r < n; r += kThreads) all += static_cast<int64_t>(tiles_of<ChunkShape>(p, request_of(p, r, &flags), rows, keys)) * keys;
+  block_scan<int64_t>(all, sums, before64, all);
   if (flags && p.status && blockIdx.x == 0) atomicOr(p.status, flags);
-  const int64_t pieces = static_cast<int64_t>(blocks) * Shape::kPieces;
-  int size = static_cast<int>(max(int64_t(1), (all + pieces - 1) / pieces));
+  int size = static_cast<int>(max(int64_t(1), (all * p.cache.kv_heads + blocks - 1) / blocks));
   for (int round = 0; round < 6; ++round) {      // last pieces that are short make it more than there is room for: take longer ones
     int64_t units = 0;
     for (int r = threadIdx.x; r < n; r += kThreads) {
-      work(r, tiles, keys, rows);
-      units += static_cast<int64_t>(tiles) * max(1, (keys + size - 1) / size);
+      const int tiles = tiles_of<ChunkShape>(p, request_of(p, r, &flags), rows, keys);
+      units += static_cast<int64_t>(tiles) * ((keys + size - 1) / size);
     }
-    if (block_sum(units, sums) * p.cache.kv_heads <= pieces) break;
+    block_scan<int64_t>(units, sums, before64, units);
+    if (units * p.cache.kv_heads <= blocks) break;
     size += size / 8 + 1;
   }
   int done[3] = {0, 0, 0};
@@ -129,8 +164,7 @@ __device__ __forceinline__ void share_out(const AttentionParams &p, const Plan &
     const int r = r0 + threadIdx.x;
     int v[3] = {0, 0, 0};
     if (r < n) {
-      work(r, tiles, keys, rows);
-      const int splits = max(1, (keys + size - 1) / size);
+      const int tiles = tiles_of<ChunkShape>(p, request_of(p, r, &flags), rows, keys), splits = (keys + size - 1) / size;
       v[0] = tiles * splits;
       v[1] = tiles && splits > 1 ? rows * splits : 0;
       v[2] = v[1] ? rows : 0;
@@ -139,7 +173,7 @@ __device__ __forceinline__ void share_out(const AttentionParams &p, const Plan &
 #pragma unroll
     for (int i = 0; i < 3; ++i) {
       int before, total;
-      block_scan(v[i], scratch, before, total);
+      block_scan<int>(v[i], scratch, before, total);
       if (r < n) to[i][r] = done[i] + before;
       done[i] += total;
     }
@@ -153,7 +187,8 @@ __device__ __forceinline__ void share_out(const AttentionParams &p, const Plan &
 }
 
 // The last of n + 1 ascending numbers' first n that is not above `at`.
-__device__ __forceinline__ int last_not_above(const int *numbers, int n, int at)
+template <class V>
+__device__ __forceinline__ int last_not_above(const V *numbers, int n, V at)
 {
   int r = 0;
   for (int step = ITER_MAX_REQUESTS / 2; step; step /= 2)
@@ -161,32 +196,24 @@ __device__ __forceinline__ int last_not_above(const int *numbers, int n, int at)
   return r;
 }
 
-// Plans as they are kept in the workspace for the kernel that joins: start, part and join of each kernel.
+// Plans as they are kept in the workspace for the kernel that joins (and what it copies to shared memory).
 __device__ __forceinline__ int *kept_plan(const AttentionParams &p, int which) { return reinterpret_cast<int *>(p.workspace) + which * 3 * (p.batch.requests + 1); }
 
-__device__ __forceinline__ void keep_plan(const AttentionParams &p, const Plan &plan, int which)
+__device__ __forceinline__ void copy_plan(const AttentionParams &p, int *to, const int *from)
 {
-  int *to = kept_plan(p, which);
-  const int n = p.batch.requests + 1;
-  for (int r = threadIdx.x; r < n; r += kThreads) {
-    to[r] = plan.start[r];
-    to[n + r] = plan.part[r];
-    to[2 * n + r] = plan.join[r];
-  }
+  for (int i = threadIdx.x; i < 3 * (p.batch.requests + 1); i += kThreads) to[i] = from[i];
 }
 
-// Units of a request: the pieces of a tile one after the other; a chunk's last tokens, which see the most keys, go first.
-template <class Shape>
-__device__ __forceinline__ int tile_of_unit(int unit, int tiles, int splits)
-{
-  return Shape::kPlan == ChunkShape::kPlan ? tiles - 1 - unit / splits : unit / splits;
-}
+// Units of a chunk: the pieces of a tile one after the other; the last tokens, which see the most keys, go first.
+__device__ __forceinline__ int tile_of_unit(int unit, int tiles, int splits) { return tiles - 1 - unit / splits; }
 
-// Whether a unit (times kv head) met something that it leaves to the kernel that joins, which computes the rows of its tile again: a
+// Marks: whether a unit met something that it leaves to the kernel that joins, which computes the rows of its tile again: a
 // page that is not there, or values that its products cannot hide from the rows that do not see them.
-__device__ __forceinline__ void mark_unit(const AttentionParams &p, int which, int64_t unit, int again)
+__device__ __forceinline__ int *marks_of(const AttentionParams &p, int which) { return reinterpret_cast<int *>(p.workspace) + p.marks[which]; }
+
+__device__ __forceinline__ void mark(const AttentionParams &p, int which, int64_t unit, int again)
 {
-  if (unit < p.units[which]) reinterpret_cast<int *>(p.workspace)[p.marks[which] + unit] = again;
+  if (unit < p.units[which]) marks_of(p, which)[unit] = again;
 }
 
 // Whether any of the pages that hold keys [from, to) is not there; they are looked at by the whole workgroup. The kernels read another page in its place.
@@ -201,9 +228,9 @@ __device__ __forceinline__ int missing_page(const AttentionParams &p, const int3
 __device__ __forceinline__ int usable_page(const AttentionParams &p, int page) { return static_cast<uint32_t>(page) < static_cast<uint32_t>(p.cache.pages) ? page : 0; }
 
 // Where a row's results go when its keys were shared out: the sum of weighted values, relative to the maximum, then maximum and sum.
-__device__ __forceinline__ float *part_of(const AttentionParams &p, int which, int64_t row, int head)
+__device__ __forceinline__ float *part_of(const AttentionParams &p, int which, int64_t row)
 {
-  return p.workspace + p.parts[which] + (row * p.cache.kv_heads + head) * (p.cache.head_dim + kPartTail);
+  return p.workspace + p.parts[which] + row * (p.cache.head_dim + kPartTail);
 }
 
 // Four elements of an output row from d on: weighted values over the sum of the weights, zeros where no key was seen.
@@ -216,6 +243,8 @@ __device__ __forceinline__ void write_row(const AttentionParams &p, int64_t toke
   w[1] = T::narrow2(o[2] * f, o[3] * f);
   *reinterpret_cast<u32x2 *>(static_cast<uint16_t *>(p.out.data) + token * p.out.token_stride + head * p.out.head_stride + d) = w;
 }
+
+constexpr size_t plan_bytes(int requests) { return (static_cast<size_t>(requests) + 1) * 3 * sizeof(int); }
 
 int launch_attention_rows(const AttentionParams &p, hipStream_t stream);
 int launch_attention_chunk(const AttentionParams &p, hipStream_t stream);

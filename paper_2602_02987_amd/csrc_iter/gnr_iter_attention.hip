@@ -65,14 +65,72 @@ __device__ __forceinline__ void one_row(const AttentionParams &p, int r, const R
   for (int i = 0; i < kMine; ++i) out[i] = static_cast<uint16_t>(T::narrow2(acc[i] * f, 0.0f));
 }
 
-// The rows of marked units, a wave for a row.
-template <class T, int kDim, class Shape>
-__device__ __forceinline__ void marked_rows(const AttentionParams &p, int *starts)
+// Adds a part of a row to those before, four elements to a lane.
+template <int kDim>
+__device__ __forceinline__ void add_part(const float *from, int lane, float &top, float &sum, f32x4 &o)
 {
-  if (!p.blocks[Shape::kPlan]) return;
+  const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 4 * lane);
+  const float m = from[kDim], l = from[kDim + 1], next = fmaxf(top, m);
+  const float a = __builtin_amdgcn_exp2f(top - next), b = __builtin_amdgcn_exp2f(m - next);
+  top = next;
+  sum = sum * a + l * b;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) o[k] = o[k] * a + x[k] * b;
+}
+
+// What the kernel for few rows left: every (tile, kv head) that was cut is joined from its parts, and one that is marked computed again. A
+// workgroup takes one at a time, a group of lanes a row.
+template <class T, int kDim>
+__device__ __forceinline__ void finish_rows(const AttentionParams &p, int64_t *memory)
+{
+  constexpr int kLanes = kDim / 4, kGroups = kThreads / kLanes, which = RowsShape::kPlan;
+  const int n = p.batch.requests, kv_heads = p.cache.kv_heads, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  copy_plan(p, reinterpret_cast<int *>(memory), kept_plan(p, which));
+  __syncthreads();
+  RowsPlan plan{memory, reinterpret_cast<int *>(memory + n + 1), memory[n] * kv_heads, 0};
+  plan.blocks = static_cast<int>(min(plan.total, static_cast<int64_t>(p.blocks[which])));
+  const int *marks = marks_of(p, which);
+  const int64_t items = static_cast<int64_t>(plan.tiles[n]) * kv_heads;
+  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+    const int r = last_not_above<int>(plan.tiles, n, static_cast<int>(item / kv_heads));
+    uint32_t flags = 0;
+    const Request rq = request_of(p, r, &flags);
+    int all_rows, blocks;
+    tiles_of<RowsShape>(p, rq, all_rows, blocks);
+    const int64_t nth = item - static_cast<int64_t>(plan.tiles[r]) * kv_heads, begin = plan.start[r] * kv_heads + nth * blocks;
+    const int tile = static_cast<int>(nth / kv_heads), head = static_cast<int>(nth % kv_heads), rows = min(16, all_rows - tile * 16);
+    const int first = plan.block_of(begin), last = plan.block_of(begin + blocks - 1);
+    const auto slot = [&](int b) { return 2 * static_cast<int64_t>(b) + (b == first); };
+    bool marked = false;
+    if (first == last) {
+      const int64_t at = 2 * static_cast<int64_t>(p.blocks[which]) + item;
+      marked = at < p.units[which] && marks[at];
+    } else {
+      for (int b = first; b <= last; ++b) marked |= marks[slot(b)] != 0;
+    }
+    if (marked) {
+      for (int y = threadIdx.x / 64; y < rows; y += kWaves) one_row<T, kDim>(p, r, rq, tile * 16 + y, head);
+    } else if (first != last) {
+      for (int y = group; y < rows; y += kGroups) {
+        float top = -FLT_MAX, sum = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+        for (int b = first; b <= last; ++b) add_part<kDim>(part_of(p, which, slot(b) * RowsShape::kRows + y), lane, top, sum, o);
+        const int row = tile * 16 + y;
+        write_row<T>(p, rq.first + row / p.group, head * p.group + row % p.group, 4 * lane, o, sum);
+      }
+    }
+  }
+}
+
+// What the kernel for chunks left: the rows of marked units, a wave for a row ...
+template <class T, int kDim>
+__device__ __forceinline__ void marked_chunks(const AttentionParams &p, int *starts)
+{
+  constexpr int which = ChunkShape::kPlan;
   const int n = p.batch.requests;
-  const int *start = kept_plan(p, Shape::kPlan), *marks = reinterpret_cast<const int *>(p.workspace) + p.marks[Shape::kPlan];
-  const int64_t units = min(p.units[Shape::kPlan], static_cast<int64_t>(start[n]) * p.cache.kv_heads);
+  const int *start = kept_plan(p, which), *marks = marks_of(p, which);
+  const int64_t units = min(p.units[which], static_cast<int64_t>(start[n]) * p.cache.kv_heads);
   bool any = false;
   for (int64_t u = blockIdx.x + static_cast<int64_t>(threadIdx.x) * gridDim.x; u < units; u += static_cast<int64_t>(kThreads) * gridDim.x) any |= marks[u] != 0;
   if (!__syncthreads_or(any)) return;
@@ -81,31 +139,28 @@ __device__ __forceinline__ void marked_rows(const AttentionParams &p, int *start
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     if (!marks[u]) continue;
     const int unit = static_cast<int>(u / p.cache.kv_heads), head = static_cast<int>(u % p.cache.kv_heads);
-    const int r = last_not_above(starts, n, unit);
+    const int r = last_not_above<int>(starts, n, unit);
     uint32_t flags = 0;
     const Request rq = request_of(p, r, &flags);
-    const int rows = rq.tokens * p.group, tiles = (rows + Shape::kRows - 1) / Shape::kRows, splits = (starts[r + 1] - starts[r]) / tiles;
-    const int tile = tile_of_unit<Shape>(unit - starts[r], tiles, splits), first = (unit - starts[r]) / splits * splits;
+    const int rows = rq.tokens * p.group, tiles = (rows + ChunkShape::kRows - 1) / ChunkShape::kRows, splits = (starts[r + 1] - starts[r]) / tiles;
+    const int tile = tile_of_unit(unit - starts[r], tiles, splits), first = (unit - starts[r]) / splits * splits;
     // of the marked pieces of a tile the first one's workgroup computes its rows
     bool before = false;
     for (int s = first; s < unit - starts[r]; ++s) before |= marks[static_cast<int64_t>(starts[r] + s) * p.cache.kv_heads + head] != 0;
     if (before) continue;
-    for (int row = tile * Shape::kRows + threadIdx.x / 64; row < min(rows, (tile + 1) * Shape::kRows); row += kWaves) one_row<T, kDim>(p, r, rq, row, head);
+    for (int row = tile * ChunkShape::kRows + threadIdx.x / 64; row < min(rows, (tile + 1) * ChunkShape::kRows); row += kWaves) one_row<T, kDim>(p, r, rq, row, head);
   }
 }
 
-// The parts of rows whose keys were shared out: a workgroup for a row at a time; groups of lanes take every eighth (head_dim 128) part
-// of it, a lane four elements.
-template <class T, int kDim, class Shape>
-__device__ __forceinline__ void join_rows(const AttentionParams &p, int *joins)
+// ... and rows whose keys were cut: a workgroup for a row at a time, every group of lanes with a share of its parts.
+template <class T, int kDim>
+__device__ __forceinline__ void join_chunks(const AttentionParams &p, int *joins)
 {
-  constexpr int kLanes = kDim / 4, kGroups = kThreads / kLanes, which = Shape::kPlan;
+  constexpr int kLanes = kDim / 4, kGroups = kThreads / kLanes, which = ChunkShape::kPlan;
   __shared__ float tops[kGroups], sums[kGroups];
   __shared__ f32x4 outs[kGroups][kLanes];
-  if (!p.blocks[which]) return;
   const int n = p.batch.requests, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  const int *start = kept_plan(p, which), *part = start + n + 1, *join = part + n + 1;
-  const int *marks = reinterpret_cast<const int *>(p.workspace) + p.marks[which];
+  const int *start = kept_plan(p, which), *part = start + n + 1, *join = part + n + 1, *marks = marks_of(p, which);
   const int64_t items = static_cast<int64_t>(join[n]) * p.cache.kv_heads;
   if (items == 0) return;
   __syncthreads();
@@ -113,26 +168,19 @@ __device__ __forceinline__ void join_rows(const AttentionParams &p, int *joins)
   __syncthreads();
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
     const int head = static_cast<int>(item % p.cache.kv_heads), at = static_cast<int>(item / p.cache.kv_heads);
-    const int r = last_not_above(joins, n, at), row = at - joins[r], rows = joins[r + 1] - joins[r];
+    const int r = last_not_above<int>(joins, n, at), row = at - joins[r], rows = joins[r + 1] - joins[r];
     const int64_t first = part[r];
-    const int splits = (part[r + 1] - part[r]) / rows, tiles = (rows + Shape::kRows - 1) / Shape::kRows, tile = row / Shape::kRows;
-    const int64_t unit = start[r] + static_cast<int64_t>(Shape::kPlan == ChunkShape::kPlan ? tiles - 1 - tile : tile) * splits;
+    const int splits = (part[r + 1] - part[r]) / rows, tiles = (rows + ChunkShape::kRows - 1) / ChunkShape::kRows;
+    const int64_t unit = start[r] + static_cast<int64_t>(tiles - 1 - row / ChunkShape::kRows) * splits;
     uint32_t flags = 0;
     const Request rq = request_of(p, r, &flags);
     float top = -FLT_MAX, sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     int marked = 0;
     for (int s = group; s < splits; s += kGroups) {
-      const float *from = part_of(p, which, first + static_cast<int64_t>(s) * rows + row, head);
-      const f32x4 x = *reinterpret_cast<const f32x4 *>(from + 4 * lane);
+      add_part<kDim>(part_of(p, which, (first + static_cast<int64_t>(s) * rows + row) * p.cache.kv_heads + head), lane, top, sum, o);
       const int64_t mark = (unit + s) * p.cache.kv_heads + head;
       if (mark < p.units[which]) marked |= marks[mark];
-      const float m = from[kDim], l = from[kDim + 1], next = fmaxf(top, m);
-      const float a = __builtin_amdgcn_exp2f(top - next), b = __builtin_amdgcn_exp2f(m - next);
-      top = next;
-      sum = sum * a + l * b;
-#pragma unroll
-      for (int k = 0; k < 4; ++k) o[k] = o[k] * a + x[k] * b;
     }
     marked = __syncthreads_or(marked);
     if (lane == 0) {
@@ -159,14 +207,16 @@ __device__ __forceinline__ void join_rows(const AttentionParams &p, int *joins)
   }
 }
 
-template <class T, int kDim>
-__global__ void __launch_bounds__(kThreads) gnr_attention_join_kernel(const AttentionParams p)
+template <class T, int kDim, bool kChunks>
+__global__ void __launch_bounds__(kThreads, 4) gnr_attention_join_kernel(const AttentionParams p)
 {
-  extern __shared__ int numbers[];
-  join_rows<T, kDim, RowsShape>(p, numbers);
-  join_rows<T, kDim, ChunkShape>(p, numbers);
-  marked_rows<T, kDim, RowsShape>(p, numbers);
-  marked_rows<T, kDim, ChunkShape>(p, numbers);
+  extern __shared__ int64_t memory[];
+  if constexpr (kChunks) {
+    join_chunks<T, kDim>(p, reinterpret_cast<int *>(memory));
+    marked_chunks<T, kDim>(p, reinterpret_cast<int *>(memory));
+  } else {
+    finish_rows<T, kDim>(p, memory);
+  }
 }
 
 // Fills in what the host decides: which kernel takes which requests, how many workgroups each has, and where its parts lie. Returns
@@ -186,20 +236,22 @@ static int64_t decide(AttentionParams &p)
     const int64_t units = (p.batch.requests + rows / tile) * ((keys + block - 1) / block + 1) * p.cache.kv_heads;
     return !used ? 0 : units < most ? units : most;
   };
-  p.blocks[0] = static_cast<int>(blocks(few, kComputeUnits * rows_blocks(p.cache.head_dim, p.cache.type == ITER_FP8), RowsShape::kRows, RowsShape::kKeys));
+  p.blocks[0] = static_cast<int>(blocks(few, kComputeUnits * rows_blocks(p.cache.head_dim), RowsShape::kRows, RowsShape::kKeys));
   p.blocks[1] = static_cast<int>(blocks(chunks, kComputeUnits * chunk_blocks(p.cache.head_dim), ChunkShape::kRows, ChunkShape::kKeys));
-  // Units: what the pieces fill, and one more for each tile. A request that is shared out has fewer than twice as many pieces as
-  // its keys fill, and only those leave parts.
-  const int64_t words = p.cache.head_dim + kPartTail;
+  // Marks of the kernel for few rows: two slots to a workgroup and every (tile, head); of the one for chunks: units, as many as there are
+  // workgroups and one more for each tile. Parts: of the former the slots' rows; of the latter, a request that is cut has fewer than
+  // twice as many pieces as its keys fill.
+  const int64_t words = p.cache.head_dim + kPartTail, heads = p.cache.kv_heads;
   int64_t at = (6 * static_cast<int64_t>(p.batch.requests + 1) + 15) / 16 * 16;
-  const int64_t pieces[2] = {static_cast<int64_t>(p.blocks[0]) * RowsShape::kPieces, static_cast<int64_t>(p.blocks[1]) * ChunkShape::kPieces};
-  const int64_t tile[2] = {RowsShape::kRows, ChunkShape::kRows};
+  const int64_t units[2] = {2 * static_cast<int64_t>(p.blocks[0]) + (p.batch.requests + rows / RowsShape::kRows) * heads,
+                            p.blocks[1] + (p.batch.requests + rows / ChunkShape::kRows) * heads};
+  const int64_t parts[2] = {2 * static_cast<int64_t>(p.blocks[0]) * RowsShape::kRows, 2 * static_cast<int64_t>(p.blocks[1]) * ChunkShape::kRows};
   for (int i = 0; i < 2; ++i) {
     p.marks[i] = at;
-    p.units[i] = p.blocks[i] ? pieces[i] + (p.batch.requests + rows / tile[i]) * p.cache.kv_heads : 0;
+    p.units[i] = p.blocks[i] ? units[i] : 0;
     at += (p.units[i] + 15) / 16 * 16;
     p.parts[i] = at;
-    at += 2 * pieces[i] * tile[i] * words;
+    at += parts[i] * words;
   }
   return at;
 }
@@ -214,17 +266,18 @@ size_t attention_bytes(const iter_cache &c, const iter_batch &b, int heads)
   return static_cast<size_t>(decide(p)) * sizeof(float);
 }
 
-template <class T>
-static void launch_join(const AttentionParams &p, hipStream_t stream)
+template <class T, bool kChunks>
+static int launch_join(const AttentionParams &p, hipStream_t stream)
 {
-  const size_t lds = static_cast<size_t>(p.batch.requests + 1) * sizeof(int);
+  const size_t lds = plan_bytes(p.batch.requests);
   const int64_t items = p.batch.tokens * p.group * p.cache.kv_heads;
   const unsigned blocks = static_cast<unsigned>(items < kJoinBlocks ? items : kJoinBlocks);
   switch (p.cache.head_dim) {
-    case 64: gnr_attention_join_kernel<T, 64><<<blocks, kThreads, lds, stream>>>(p); break;
-    case 128: gnr_attention_join_kernel<T, 128><<<blocks, kThreads, lds, stream>>>(p); break;
-    default: gnr_attention_join_kernel<T, 256><<<blocks, kThreads, lds, stream>>>(p); break;
+    case 64: gnr_attention_join_kernel<T, 64, kChunks><<<blocks, kThreads, lds, stream>>>(p); break;
+    case 128: gnr_attention_join_kernel<T, 128, kChunks><<<blocks, kThreads, lds, stream>>>(p); break;
+    default: gnr_attention_join_kernel<T, 256, kChunks><<<blocks, kThreads, lds, stream>>>(p); break;
   }
+  return iter_hip_ok(hipGetLastError());
 }
 
 int launch_attention(const AttentionParams &params, void *stream)
@@ -235,10 +288,9 @@ int launch_attention(const AttentionParams &params, void *stream)
   int rc = SIM_OK;
   if (p.blocks[0]) rc = launch_attention_rows(p, s);
   if (rc == SIM_OK && p.blocks[1]) rc = launch_attention_chunk(p, s);
-  if (rc != SIM_OK) return rc;
-  if (p.type == ITER_BF16) launch_join<Bf16>(p, s);
-  else launch_join<Fp16>(p, s);
-  return iter_hip_ok(hipGetLastError());
+  if (rc == SIM_OK && p.blocks[0]) rc = p.type == ITER_BF16 ? launch_join<Bf16, false>(p, s) : launch_join<Fp16, false>(p, s);
+  if (rc == SIM_OK && p.blocks[1]) rc = p.type == ITER_BF16 ? launch_join<Bf16, true>(p, s) : launch_join<Fp16, true>(p, s);
+  return rc;
 }
 
 }  // namespace gnr

@@ -170,9 +170,9 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
   extern __shared__ int shared[];
   __shared__ __attribute__((aligned(16))) char keys[2 * kKeys * kRowBytes], values[2 * kKeys * kRowBytes];
   const int requests = p.batch.requests, kv_heads = p.cache.kv_heads;
-  const Plan plan{shared, shared + requests + 1, shared + 2 * (requests + 1)};
-  share_out<ChunkShape>(p, plan, gridDim.x);
-  if (blockIdx.x == 0) keep_plan(p, plan, ChunkShape::kPlan);
+  const ChunkPlan plan{shared, shared + requests + 1, shared + 2 * (requests + 1)};
+  share_out_chunks(p, plan, gridDim.x);
+  if (blockIdx.x == 0) copy_plan(p, kept_plan(p, ChunkShape::kPlan), shared);
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   const int n = lane % 32, h = lane / 32;
   Loader<T, kDim, kFp8, kSmallPages> key_loader(p.cache.k, wave, lane), value_loader(p.cache.v, wave, lane);
@@ -184,12 +184,12 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
     const int64_t u = round * gridDim.x + (round % 2 ? back * dealt + blockIdx.x % dealt : blockIdx.x);
     if (u >= units) continue;
     const int unit = static_cast<int>(u / kv_heads), head = static_cast<int>(u % kv_heads);
-    const int r = __builtin_amdgcn_readfirstlane(last_not_above(plan.start, requests, unit));
+    const int r = uniform(last_not_above<int>(plan.start, requests, unit));
     uint32_t flags = 0;
     const Request rq = request_of(p, r, &flags);
     const int all_rows = rq.tokens * p.group, tiles = (all_rows + ChunkShape::kRows - 1) / ChunkShape::kRows;
-    const int splits = __builtin_amdgcn_readfirstlane(plan.start[r + 1] - plan.start[r]) / tiles, local = unit - __builtin_amdgcn_readfirstlane(plan.start[r]);
-    const int tile = tile_of_unit<ChunkShape>(local, tiles, splits), split = local % splits;
+    const int splits = uniform(plan.start[r + 1] - plan.start[r]) / tiles, local = unit - uniform(plan.start[r]);
+    const int tile = tile_of_unit(local, tiles, splits), split = local % splits;
     const int32_t *table = p.batch.page_table + r * p.batch.table_stride;
     // the keys that a row sees end before end_of and begin at begin_of
     const auto pos_of = [&](int row) { return rq.base + min(row, all_rows - 1) / p.group; };
@@ -349,12 +349,12 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
       add(std::false_type{}, w);
     }
     again = __syncthreads_or(again);                            // (and nobody reads the last block any more)
-    if (threadIdx.x == 0) mark_unit(p, ChunkShape::kPlan, u, again);
+    if (threadIdx.x == 0) mark(p, ChunkShape::kPlan, u, again);
     sum += __shfl_xor(sum, 32);
     if (row < all_rows) {
       const int64_t token = rq.first + row / p.group;
       const int64_t part_row = static_cast<int64_t>(plan.part[r]) + static_cast<int64_t>(split) * all_rows + row;
-      float *part = part_of(p, ChunkShape::kPlan, part_row, head);
+      float *part = part_of(p, ChunkShape::kPlan, part_row * kv_heads + head);
 #pragma unroll
       for (int e = 0; e < kTiles; ++e)
 #pragma unroll
@@ -376,7 +376,7 @@ template <class T, int kDim, bool kFp8>
 static int launch(const AttentionParams &p, hipStream_t stream)
 {
   const unsigned blocks = static_cast<unsigned>(p.blocks[ChunkShape::kPlan]);
-  const size_t lds = static_cast<size_t>(p.batch.requests + 1) * 3 * sizeof(int);
+  const size_t lds = plan_bytes(p.batch.requests);
   if (p.cache.page < 16) gnr_attention_chunk_kernel<T, kDim, kFp8, true><<<blocks, kThreads, lds, stream>>>(p);
   else gnr_attention_chunk_kernel<T, kDim, kFp8, false><<<blocks, kThreads, lds, stream>>>(p);
   return iter_hip_ok(hipGetLastError());

@@ -232,33 +232,37 @@ struct Tile {
 };
 
 template <class T, int kDim, bool kFp8, bool kSmallPages>
-__global__ void __launch_bounds__(kThreads, rows_blocks(kDim, kFp8)) gnr_attention_rows_kernel(const AttentionParams p)
+__global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_rows_kernel(const AttentionParams p)
 {
   typedef Tile<T, kDim, kFp8, kSmallPages> Rows;
-  extern __shared__ int shared[];
+  extern __shared__ int64_t shared[];
   __shared__ float tops[kWaves][16], sums[kWaves][16];
   __shared__ float outs[kWaves][16][kDim + 4];
   const int requests = p.batch.requests, kv_heads = p.cache.kv_heads;
-  const Plan plan{shared, shared + requests + 1, shared + 2 * (requests + 1)};
-  share_out<RowsShape>(p, plan, gridDim.x);
-  if (blockIdx.x == 0) keep_plan(p, plan, RowsShape::kPlan);
+  const RowsPlan plan = share_out_rows(p, shared, gridDim.x);
+  if (blockIdx.x == 0) copy_plan(p, kept_plan(p, RowsShape::kPlan), reinterpret_cast<const int *>(shared));
+  if (static_cast<int>(blockIdx.x) >= plan.blocks) return;
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Rows rows(lane);
-  const int64_t units = static_cast<int64_t>(plan.start[requests]) * kv_heads;
-  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int unit = static_cast<int>(u / kv_heads), head = static_cast<int>(u % kv_heads);
-    const int r = __builtin_amdgcn_readfirstlane(last_not_above(plan.start, requests, unit));
+  const int64_t cut = plan.cut(blockIdx.x + 1);
+  int began_before = 0, ends_after = 0;                         // marks of the two slots
+  for (int64_t x = plan.cut(blockIdx.x); x < cut;) {
+    const int r = uniform(last_not_above<int64_t>(plan.start, requests, x / kv_heads));
     uint32_t flags = 0;
     const Request rq = request_of(p, r, &flags);
-    const int all_rows = rq.tokens * p.group, tiles = (all_rows + 15) / 16;
-    const int splits = __builtin_amdgcn_readfirstlane(plan.start[r + 1] - plan.start[r]) / tiles, local = unit - __builtin_amdgcn_readfirstlane(plan.start[r]);
-    const int tile = tile_of_unit<RowsShape>(local, tiles, splits), split = local % splits;
-    const int blocks = (rq.end - rq.begin + RowsShape::kKeys - 1) / RowsShape::kKeys, each = (blocks + splits - 1) / splits;
+    int all_rows, blocks;
+    tiles_of<RowsShape>(p, rq, all_rows, blocks);
+    // the (tile, head) that x is in, its blocks of keys from `first` to `last`, and whether these are all
+    const int64_t local = x - uniform(plan.start[r]) * kv_heads;
+    const int nth = static_cast<int>(local / blocks), tile = nth / kv_heads, head = nth % kv_heads;
+    const int first = static_cast<int>(local - static_cast<int64_t>(nth) * blocks);
+    const int last = static_cast<int>(min(static_cast<int64_t>(blocks), first + (cut - x)));
+    const bool whole = first == 0 && last == blocks;
+    x += last - first;
     // what the tile's tokens see: the last one's end, and what all of them see
     const int first_pos = rq.base + tile * 16 / p.group, last_pos = rq.base + min(rq.tokens - 1, (tile * 16 + 15) / p.group);
     const int all_end = min(first_pos + 1, rq.end), all_begin = p.window ? last_pos - p.window + 1 : 0;
-    const int from = rq.begin + min(blocks, split * each) * RowsShape::kKeys;
-    const int stop = min(min(rq.end, last_pos + 1), rq.begin + min(blocks, (split + 1) * each) * RowsShape::kKeys);
+    const int from = rq.begin + first * RowsShape::kKeys, stop = min(min(rq.end, last_pos + 1), rq.begin + last * RowsShape::kKeys);
     const int32_t *table = p.batch.page_table + r * p.batch.table_stride;
     const int row = min(tile * 16 + rows.n, all_rows - 1), pos = rq.base + row / p.group;   // (rows beyond the last repeat it; nobody reads them)
     rows.begin(p, head, static_cast<const uint16_t *>(p.q.data) + static_cast<int64_t>(rq.first + row / p.group) * p.q.token_stride + (head * p.group + row % p.group) * p.q.head_stride);
@@ -321,7 +325,13 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim, kFp8)) gnr_attenti
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     again = __syncthreads_or(again);                             // (the unit before has been read)
-    if (threadIdx.x == 0) mark_unit(p, RowsShape::kPlan, u, again);
+    if (whole) {
+      if (threadIdx.x == 0) mark(p, RowsShape::kPlan, 2 * gridDim.x + (static_cast<int64_t>(plan.tiles[r]) + tile) * kv_heads + head, again);
+    } else if (first == 0) {
+      ends_after = again;
+    } else {
+      began_before = again;
+    }
     if (rows.g == 0) {
       tops[wave][rows.n] = rows.top;
       sums[wave][rows.n] = sum;
@@ -347,10 +357,10 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim, kFp8)) gnr_attenti
         for (int k = 0; k < 4; ++k) o[k] = __builtin_fmaf(outs[w][y][d + k], f, o[k]);
       }
       const int at = tile * 16 + y;
-      if (splits == 1) {
+      if (whole) {
         write_row<T>(p, rq.first + at / p.group, head * p.group + at % p.group, d, o, all);
       } else {
-        float *to_part = part_of(p, RowsShape::kPlan, static_cast<int64_t>(plan.part[r]) + static_cast<int64_t>(split) * all_rows + at, head);
+        float *to_part = part_of(p, RowsShape::kPlan, (2 * static_cast<int64_t>(blockIdx.x) + (first == 0)) * RowsShape::kRows + y);
         *reinterpret_cast<f32x4 *>(to_part + d) = o;
         if (d == 0) {
           to_part[kDim] = most;
@@ -359,13 +369,14 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim, kFp8)) gnr_attenti
       }
     }
   }
+  if (threadIdx.x < 2) mark(p, RowsShape::kPlan, 2 * blockIdx.x + threadIdx.x, threadIdx.x ? ends_after : began_before);
 }
 
 template <class T, int kDim, bool kFp8>
 static int launch(const AttentionParams &p, hipStream_t stream)
 {
   const unsigned blocks = static_cast<unsigned>(p.blocks[RowsShape::kPlan]);
-  const size_t lds = static_cast<size_t>(p.batch.requests + 1) * 3 * sizeof(int);
+  const size_t lds = plan_bytes(p.batch.requests);
   if (p.cache.page < 16) gnr_attention_rows_kernel<T, kDim, kFp8, true><<<blocks, kThreads, lds, stream>>>(p);
   else gnr_attention_rows_kernel<T, kDim, kFp8, false><<<blocks, kThreads, lds, stream>>>(p);
   return iter_hip_ok(hipGetLastError());

@@ -77,6 +77,14 @@ __device__ __forceinline__ void repeat(const F &f)
 template <class T>
 __device__ __forceinline__ bool no_number(uint32_t w) { return (w & T::kInf) == T::kInf || (w >> 16 & T::kInf) == T::kInf; }
 
+// A number that is the same in all lanes, in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(v)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(v >> 32));
+  return static_cast<int64_t>(static_cast<uint64_t>(hi) << 32 | lo);
+}
+
 // A wave's load of 64 x 16 bytes from memory to 1 KB of shared memory, lane after lane; wait_for_lds_loads waits for all of the wave's.
 __device__ __forceinline__ void load_to_lds(const void *from, char *to)
 {
