@@ -95,6 +95,12 @@ struct RowsPlan {
   __device__ __forceinline__ int block_of(int64_t x) const { return static_cast<int>(((x + 1) * blocks + total - 1) / total - 1); }
 };
 
+// What the workgroup in which a (tile, kv head) begins that is cut leaves for the join beside slot 1: where its rows are and the last workgroup with a
+// part of it. Every workgroup writes one, with `rows` = 0 if there is none.
+struct alignas(16) CutTile {
+  int rows, tile, head, request, token, last, mark[2];   // mark: of the slots 0 and 1
+};
+
 __device__ __forceinline__ RowsPlan share_out_rows(const AttentionParams &p, void *memory, int blocks)
 {
   __shared__ int64_t scratch64[kWaves];
@@ -206,6 +212,8 @@ __device__ __forceinline__ void copy_plan(const AttentionParams &p, int *to, con
 
 // Units of a chunk: the pieces of a tile one after the other; the last tokens, which see the most keys, go first.
 __device__ __forceinline__ int tile_of_unit(int unit, int tiles, int splits) { return tiles - 1 - unit / splits; }
+
+__device__ __forceinline__ CutTile *cut_tiles(const AttentionParams &p) { return reinterpret_cast<CutTile *>(p.workspace + p.cuts); }
 
 // Marks: whether a unit met something that it leaves to the kernel that joins, which computes the rows of its tile again: a
 // page that is not there, or values that its products cannot hide from the rows that do not see them.

@@ -78,48 +78,49 @@ __device__ __forceinline__ void add_part(const float *from, int lane, float &top
   for (int k = 0; k < 4; ++k) o[k] = o[k] * a + x[k] * b;
 }
 
-// What the kernel for few rows left: every (tile, kv head) that was cut is joined from its parts, and one that is marked computed again. A
-// workgroup takes one at a time, a group of lanes a row.
+// What the kernel for few rows left: a tile (of a kv head) that was cut is joined from its parts by the workgroup with the number of the one in
+// which it begins, a group of lanes a row; one that is marked is computed again.
 template <class T, int kDim>
-__device__ __forceinline__ void finish_rows(const AttentionParams &p, int64_t *memory)
+__device__ __forceinline__ void finish_rows(const AttentionParams &p)
 {
   constexpr int kLanes = kDim / 4, kGroups = kThreads / kLanes, which = RowsShape::kPlan;
   const int n = p.batch.requests, kv_heads = p.cache.kv_heads, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
-  copy_plan(p, reinterpret_cast<int *>(memory), kept_plan(p, which));
-  __syncthreads();
-  RowsPlan plan{memory, reinterpret_cast<int *>(memory + n + 1), memory[n] * kv_heads, 0};
-  plan.blocks = static_cast<int>(min(plan.total, static_cast<int64_t>(p.blocks[which])));
+  uint32_t flags = 0;
+  if (static_cast<int>(blockIdx.x) < p.blocks[which]) {
+    const int first = blockIdx.x;
+    const CutTile cut = cut_tiles(p)[first];
+    if (cut.rows) {
+      int marked = threadIdx.x == 0 ? cut.mark[1] : 0;
+      for (int b = first + 1 + static_cast<int>(threadIdx.x); b <= cut.last; b += kThreads) marked |= cut_tiles(p)[b].mark[0];
+      for (int y = group; y < cut.rows; y += kGroups) {
+        float top = -FLT_MAX, sum = 0.0f;
+        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
+        add_part<kDim>(part_of(p, which, (2 * static_cast<int64_t>(first) + 1) * RowsShape::kRows + y), lane, top, sum, o);
+#pragma unroll 4
+        for (int b = first + 1; b <= cut.last; ++b) add_part<kDim>(part_of(p, which, 2 * static_cast<int64_t>(b) * RowsShape::kRows + y), lane, top, sum, o);
+        const int row = cut.tile * 16 + y;
+        write_row<T>(p, cut.token + row / p.group, cut.head * p.group + row % p.group, 4 * lane, o, sum);
+      }
+      if (__syncthreads_or(marked)) {                           // (and what was written above is written over)
+        const Request rq = request_of(p, cut.request, &flags);
+        for (int y = threadIdx.x / 64; y < cut.rows; y += kWaves) one_row<T, kDim>(p, cut.request, rq, cut.tile * 16 + y, cut.head);
+      }
+    }
+  }
+  // tiles that were not cut
   const int *marks = marks_of(p, which);
-  const int64_t items = static_cast<int64_t>(plan.tiles[n]) * kv_heads;
+  const int64_t *start = reinterpret_cast<const int64_t *>(kept_plan(p, which));
+  const int *tiles = reinterpret_cast<const int *>(start + n + 1);
+  const int64_t items = min(p.units[which], static_cast<int64_t>(tiles[n]) * kv_heads);
   for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
-    const int r = last_not_above<int>(plan.tiles, n, static_cast<int>(item / kv_heads));
-    uint32_t flags = 0;
+    if (!marks[item]) continue;
+    const int r = last_not_above<int>(tiles, n, static_cast<int>(item / kv_heads));
     const Request rq = request_of(p, r, &flags);
     int all_rows, blocks;
     tiles_of<RowsShape>(p, rq, all_rows, blocks);
-    const int64_t nth = item - static_cast<int64_t>(plan.tiles[r]) * kv_heads, begin = plan.start[r] * kv_heads + nth * blocks;
-    const int tile = static_cast<int>(nth / kv_heads), head = static_cast<int>(nth % kv_heads), rows = min(16, all_rows - tile * 16);
-    const int first = plan.block_of(begin), last = plan.block_of(begin + blocks - 1);
-    const auto slot = [&](int b) { return 2 * static_cast<int64_t>(b) + (b == first); };
-    bool marked = false;
-    if (first == last) {
-      const int64_t at = 2 * static_cast<int64_t>(p.blocks[which]) + item;
-      marked = at < p.units[which] && marks[at];
-    } else {
-      for (int b = first; b <= last; ++b) marked |= marks[slot(b)] != 0;
-    }
-    if (marked) {
-      for (int y = threadIdx.x / 64; y < rows; y += kWaves) one_row<T, kDim>(p, r, rq, tile * 16 + y, head);
-    } else if (first != last) {
-      for (int y = group; y < rows; y += kGroups) {
-        float top = -FLT_MAX, sum = 0.0f;
-        f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 4
-        for (int b = first; b <= last; ++b) add_part<kDim>(part_of(p, which, slot(b) * RowsShape::kRows + y), lane, top, sum, o);
-        const int row = tile * 16 + y;
-        write_row<T>(p, rq.first + row / p.group, head * p.group + row % p.group, 4 * lane, o, sum);
-      }
-    }
+    const int64_t nth = item - static_cast<int64_t>(tiles[r]) * kv_heads;
+    const int tile = static_cast<int>(nth / kv_heads), head = static_cast<int>(nth % kv_heads);
+    for (int y = threadIdx.x / 64; y < min(16, all_rows - tile * 16); y += kWaves) one_row<T, kDim>(p, r, rq, tile * 16 + y, head);
   }
 }
 
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 4) gnr_attention_join_kernel(const A
     join_chunks<T, kDim>(p, reinterpret_cast<int *>(memory));
     marked_chunks<T, kDim>(p, reinterpret_cast<int *>(memory));
   } else {
-    finish_rows<T, kDim>(p, memory);
+    finish_rows<T, kDim>(p);
   }
 }
 
@@ -238,13 +239,12 @@ static int64_t decide(AttentionParams &p)
   };
   p.blocks[0] = static_cast<int>(blocks(few, kComputeUnits * rows_blocks(p.cache.head_dim), RowsShape::kRows, RowsShape::kKeys));
   p.blocks[1] = static_cast<int>(blocks(chunks, kComputeUnits * chunk_blocks(p.cache.head_dim), ChunkShape::kRows, ChunkShape::kKeys));
-  // Marks of the kernel for few rows: two slots to a workgroup and every (tile, head); of the one for chunks: units, as many as there are
+  // Marks of the kernel for few rows: every (tile, head); of the one for chunks: units, as many as there are
   // workgroups and one more for each tile. Parts: of the former the slots' rows; of the latter, a request that is cut has fewer than
   // twice as many pieces as its keys fill.
   const int64_t words = p.cache.head_dim + kPartTail, heads = p.cache.kv_heads;
   int64_t at = (6 * static_cast<int64_t>(p.batch.requests + 1) + 15) / 16 * 16;
-  const int64_t units[2] = {2 * static_cast<int64_t>(p.blocks[0]) + (p.batch.requests + rows / RowsShape::kRows) * heads,
-                            p.blocks[1] + (p.batch.requests + rows / ChunkShape::kRows) * heads};
+  const int64_t units[2] = {(p.batch.requests + rows / RowsShape::kRows) * heads, p.blocks[1] + (p.batch.requests + rows / ChunkShape::kRows) * heads};
   const int64_t parts[2] = {2 * static_cast<int64_t>(p.blocks[0]) * RowsShape::kRows, 2 * static_cast<int64_t>(p.blocks[1]) * ChunkShape::kRows};
   for (int i = 0; i < 2; ++i) {
     p.marks[i] = at;
@@ -253,7 +253,8 @@ static int64_t decide(AttentionParams &p)
     p.parts[i] = at;
     at += parts[i] * words;
   }
-  return at;
+  p.cuts = at;
+  return at + p.blocks[0] * static_cast<int64_t>(sizeof(CutTile) / sizeof(float));
 }
 
 size_t attention_bytes(const iter_cache &c, const iter_batch &b, int heads)
@@ -271,7 +272,7 @@ static int launch_join(const AttentionParams &p, hipStream_t stream)
 {
   const size_t lds = plan_bytes(p.batch.requests);
   const int64_t items = p.batch.tokens * p.group * p.cache.kv_heads;
-  const unsigned blocks = static_cast<unsigned>(items < kJoinBlocks ? items : kJoinBlocks);
+  const unsigned blocks = static_cast<unsigned>(!kChunks ? p.blocks[RowsShape::kPlan] : items < kJoinBlocks ? items : kJoinBlocks);
   switch (p.cache.head_dim) {
     case 64: gnr_attention_join_kernel<T, 64, kChunks><<<blocks, kThreads, lds, stream>>>(p); break;
     case 128: gnr_attention_join_kernel<T, 128, kChunks><<<blocks, kThreads, lds, stream>>>(p); break;

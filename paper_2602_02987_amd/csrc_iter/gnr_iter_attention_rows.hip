@@ -241,11 +241,14 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_row
   const int requests = p.batch.requests, kv_heads = p.cache.kv_heads;
   const RowsPlan plan = share_out_rows(p, shared, gridDim.x);
   if (blockIdx.x == 0) copy_plan(p, kept_plan(p, RowsShape::kPlan), reinterpret_cast<const int *>(shared));
-  if (static_cast<int>(blockIdx.x) >= plan.blocks) return;
+  CutTile cut_tile{};
+  if (static_cast<int>(blockIdx.x) >= plan.blocks) {
+    if (threadIdx.x == 0) cut_tiles(p)[blockIdx.x] = cut_tile;
+    return;
+  }
   const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
   Rows rows(lane);
   const int64_t cut = plan.cut(blockIdx.x + 1);
-  int began_before = 0, ends_after = 0;                         // marks of the two slots
   for (int64_t x = plan.cut(blockIdx.x); x < cut;) {
     const int r = uniform(last_not_above<int64_t>(plan.start, requests, x / kv_heads));
     uint32_t flags = 0;
@@ -325,12 +328,11 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_row
     sum += __shfl_xor(sum, 16);
     sum += __shfl_xor(sum, 32);
     again = __syncthreads_or(again);                             // (the unit before has been read)
-    if (whole) {
-      if (threadIdx.x == 0) mark(p, RowsShape::kPlan, 2 * gridDim.x + (static_cast<int64_t>(plan.tiles[r]) + tile) * kv_heads + head, again);
-    } else if (first == 0) {
-      ends_after = again;
-    } else {
-      began_before = again;
+    if (first == 0 && threadIdx.x == 0) mark(p, RowsShape::kPlan, (static_cast<int64_t>(plan.tiles[r]) + tile) * kv_heads + head, whole ? again : 0);
+    if (first == 0 && !whole) {
+      cut_tile = CutTile{min(16, all_rows - tile * 16), tile, head, r, rq.first, plan.block_of(x - last + blocks - 1), {cut_tile.mark[0], again}};
+    } else if (first != 0) {
+      cut_tile.mark[0] = again;
     }
     if (rows.g == 0) {
       tops[wave][rows.n] = rows.top;
@@ -369,7 +371,7 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_row
       }
     }
   }
-  if (threadIdx.x < 2) mark(p, RowsShape::kPlan, 2 * blockIdx.x + threadIdx.x, threadIdx.x ? ends_after : began_before);
+  if (threadIdx.x == 0) cut_tiles(p)[blockIdx.x] = cut_tile;
 }
 
 template <class T, int kDim, bool kFp8>

@@ -23,6 +23,7 @@ struct AttentionParams {
   int least[2], most[2], blocks[2];
   int64_t parts[2];
   int64_t marks[2], units[2];  // first word of the units' marks and how many there can be
+  int64_t cuts;                // first word of the records of cut tiles
   uint32_t *status;
 };
 
