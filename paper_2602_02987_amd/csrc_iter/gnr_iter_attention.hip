@@ -134,7 +134,7 @@ __device__ __forceinline__ void marked_chunks(const AttentionParams &p, int *sta
   const int64_t units = min(p.units[which], static_cast<int64_t>(start[n]) * p.cache.kv_heads);
   bool any = false;
   for (int64_t u = blockIdx.x + static_cast<int64_t>(threadIdx.x) * gridDim.x; u < units; u += static_cast<int64_t>(kThreads) * gridDim.x) any |= marks[u] != 0;
-  if (!__syncthreads_or(any)) return;
+  if (!__syncthreads_or(any)) return;                           // (and nobody looks at joins any more)
   for (int r = threadIdx.x; r <= n; r += kThreads) starts[r] = start[r];
   __syncthreads();
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
@@ -153,21 +153,18 @@ __device__ __forceinline__ void marked_chunks(const AttentionParams &p, int *sta
   }
 }
 
-// ... and rows whose keys were cut: a workgroup for a row at a time, every group of lanes with a share of its parts.
+// ... and rows whose keys were cut: a group of lanes for a row.
 template <class T, int kDim>
 __device__ __forceinline__ void join_chunks(const AttentionParams &p, int *joins)
 {
   constexpr int kLanes = kDim / 4, kGroups = kThreads / kLanes, which = ChunkShape::kPlan;
-  __shared__ float tops[kGroups], sums[kGroups];
-  __shared__ f32x4 outs[kGroups][kLanes];
   const int n = p.batch.requests, lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const int *start = kept_plan(p, which), *part = start + n + 1, *join = part + n + 1, *marks = marks_of(p, which);
   const int64_t items = static_cast<int64_t>(join[n]) * p.cache.kv_heads;
   if (items == 0) return;
-  __syncthreads();
   for (int r = threadIdx.x; r <= n; r += kThreads) joins[r] = join[r];
   __syncthreads();
-  for (int64_t item = blockIdx.x; item < items; item += gridDim.x) {
+  for (int64_t item = static_cast<int64_t>(blockIdx.x) * kGroups + group; item < items; item += static_cast<int64_t>(gridDim.x) * kGroups) {
     const int head = static_cast<int>(item % p.cache.kv_heads), at = static_cast<int>(item / p.cache.kv_heads);
     const int r = last_not_above<int>(joins, n, at), row = at - joins[r], rows = joins[r + 1] - joins[r];
     const int64_t first = part[r];
@@ -178,33 +175,13 @@ __device__ __forceinline__ void join_chunks(const AttentionParams &p, int *joins
     float top = -FLT_MAX, sum = 0.0f;
     f32x4 o = {0.0f, 0.0f, 0.0f, 0.0f};
     int marked = 0;
-    for (int s = group; s < splits; s += kGroups) {
+#pragma unroll 4
+    for (int s = 0; s < splits; ++s) {
       add_part<kDim>(part_of(p, which, (first + static_cast<int64_t>(s) * rows + row) * p.cache.kv_heads + head), lane, top, sum, o);
       const int64_t mark = (unit + s) * p.cache.kv_heads + head;
       if (mark < p.units[which]) marked |= marks[mark];
     }
-    marked = __syncthreads_or(marked);
-    if (lane == 0) {
-      tops[group] = top;
-      sums[group] = sum;
-    }
-    outs[group][lane] = o;
-    __syncthreads();
-    if (group == 0 && !marked) {
-      float most = top;
-#pragma unroll
-      for (int s = 1; s < kGroups; ++s) most = fmaxf(most, tops[s]);
-      float all = 0.0f;
-      o = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int s = 0; s < kGroups; ++s) {
-        const float f = __builtin_amdgcn_exp2f(tops[s] - most);
-        all = __builtin_fmaf(sums[s], f, all);
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = __builtin_fmaf(outs[s][lane][k], f, o[k]);
-      }
-      write_row<T>(p, rq.first + row / p.group, head * p.group + row % p.group, 4 * lane, o, all);
-    }
+    if (!marked) write_row<T>(p, rq.first + row / p.group, head * p.group + row % p.group, 4 * lane, o, sum);
   }
 }
 

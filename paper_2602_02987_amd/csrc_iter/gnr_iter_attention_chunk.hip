@@ -22,120 +22,110 @@ __device__ __forceinline__ int piece_of(int key, int piece)
 // pages are small; 16-bit rows go there directly, 8-bit codes by way of registers, where they are widened.
 template <class T, int kDim, bool kFp8, bool kSmallPages>
 struct Loader {
-  static constexpr int kPieces = kDim / 8, kRowBytes = kDim * 2;
-  static constexpr int kMine = ChunkShape::kKeys * kPieces / kThreads;   // pieces of a block that a thread brings in
-  static constexpr int kRows = 64 / kPieces, kStep = kWaves * kRows;     // keys of a wave's load, and those between a thread's
-  static constexpr int kSize = kFp8 ? 1 : 2;
+  static constexpr int kRowBytes = kDim * 2, kCacheBytes = kFp8 ? kDim : kDim * 2, kSize = kFp8 ? 1 : 2;
+  static constexpr int kLanes = kCacheBytes / 16;                        // lanes of a row of the cache, 16 bytes each
+  static constexpr int kRows = 64 / kLanes, kStep = kWaves * kRows;      // keys of a wave's load, and those between a thread's
+  static constexpr int kMine = ChunkShape::kKeys / kStep;                // loads of a thread for a block
   // Rows of 256 elements in 8 bits are loaded when they are due: there are no registers to hold them meanwhile.
   static constexpr bool kLate = kFp8 && kDim == 256;
   const iter_plane &plane;
-  const int wave, key, piece;                                            // this thread's first key of a block, and its place in LDS rows
+  const int wave, in, part;                                              // this thread's key of a wave's load, and its part of the row
+  const int widened_at;                                                  // where the first half of a part goes once it is widened (pieces are in the same order every 16 keys)
   const char *rows;                                                      // of the kv head
   const uint8_t *exps;
-  u32x2 codes[kFp8 ? kMine : 1];
+  u32x4 codes[kFp8 ? kMine : 1];
   uint8_t exp[kFp8 ? kMine : 1];
   int pages_ahead, next_block;                                           // pages of the sixteens of 16 blocks, a lane for each
 
-  __device__ __forceinline__ Loader(const iter_plane &c, int w, int lane) : plane(c), wave(w), key(w * kRows + lane / kPieces), piece(lane % kPieces) {}
+  __device__ __forceinline__ Loader(const iter_plane &c, int w, int lane) : plane(c), wave(w), in(lane / kLanes), part(lane % kLanes),
+                                                                                      widened_at((w * kRows + in) * kRowBytes + piece_of<kDim>(w * kRows + in, 2 * part) * 16)
+  {
+    static_assert(!kFp8 || kStep % 16 == 0, "pieces in the same order");
+  }
 
   __device__ __forceinline__ void begin(int head)
   {
     rows = static_cast<const char *>(plane.data) + head * plane.head_stride * kSize;
-    if constexpr (kFp8) exps = plane.exp + head * plane.exp_head_stride;
+    exps = kFp8 ? plane.exp + head * plane.exp_head_stride : nullptr;
     next_block = 16;
   }
 
-  // A thread's i-th piece of the block at k0: where it lies in the cache. What lies beyond `to` is any row.
-  __device__ __forceinline__ void locate(const AttentionParams &p, const int32_t *table, int k0, int to, int i, int &page, int &place) const
+  // bytes of a row that a lane reads: a 16-bit row goes to shared memory as it comes, so its pieces are put in order here
+  __device__ __forceinline__ uint32_t offset_in_row(int i) const { return kFp8 ? part * 16 : piece_of<kDim>(i * kStep + wave * kRows + in, part) * 16; }
+
+  __device__ __forceinline__ void fetch(int i, const char *row, const uint8_t *e, char *lds)
   {
-    const int row0 = i * kStep + wave * kRows, in = key - wave * kRows;   // of the block
-    if constexpr (kSmallPages) {
-      const int at = min(k0 + row0 + in, to - 1);
-      page = usable_page(p, table[at >> p.page_shift]);
-      place = at & (p.cache.page - 1);
+    if constexpr (kFp8) {
+      codes[i] = *reinterpret_cast<const u32x4 *>(row);
+      exp[i] = *e;
     } else {
-      page = __builtin_amdgcn_readlane(pages_ahead, 4 * next_block + row0 / 16);
-      place = ((k0 + row0) & (p.cache.page - 1)) + in;
+      load_to_lds(row, lds + (i * kStep + wave * kRows) * kRowBytes);
     }
   }
 
-  __device__ __forceinline__ void look_up(const AttentionParams &p, const int32_t *table, int k0, int to)
+  // Loads the block of keys from k0 on; what lies beyond `to` is any row of the cache.
+  __device__ __forceinline__ void load(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
   {
-    if constexpr (!kSmallPages) {
+    if constexpr (kSmallPages) {
+#pragma unroll
+      for (int i = 0; i < kMine; ++i) {
+        const int key = min(k0 + i * kStep + wave * kRows + in, to - 1), place = key & (p.cache.page - 1);
+        const int64_t page = usable_page(p, table[key >> p.page_shift]);
+        fetch(i, rows + (page * plane.page_stride + place * plane.place_stride) * kSize + offset_in_row(i), kFp8 ? exps + page * plane.exp_page_stride + place * plane.exp_place_stride : nullptr, lds);
+      }
+    } else {
       if (next_block == 16) {
         const int at = min(k0 + 16 * static_cast<int>(threadIdx.x % 64), to - 1);
         pages_ahead = usable_page(p, table[at >> p.page_shift]);
         next_block = 0;
       }
-    }
-  }
-
-  __device__ __forceinline__ void load_codes(int page, int place, int i)
-  {
-    codes[i] = *reinterpret_cast<const u32x2 *>(rows + page * plane.page_stride + place * plane.place_stride + piece * 8);
-    exp[i] = exps[page * plane.exp_page_stride + place * plane.exp_place_stride];
-  }
-
-  // Starts on the block of keys from k0 on.
-  __device__ __forceinline__ void bring(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
-  {
-    if constexpr (kLate) return;
-    look_up(p, table, k0, to);
-    if constexpr (!kFp8 && !kSmallPages) {
-      // Addresses in scalar registers but for what does not change: the row within a load's and the piece. A wave issues one instruction
+      // Addresses in scalar registers but for what does not change: the row within a load's and the part of it. A wave issues one instruction
       // at a time, and this runs beside the products.
-      constexpr int kPeriod = 16 / kStep > 1 ? 16 / kStep : 1;           // loads until the order of pieces repeats
+      constexpr int kPeriod = kFp8 || kStep >= 16 ? 1 : 16 / kStep;       // loads until the order of pieces repeats
       uint32_t offset[kPeriod];
 #pragma unroll
-      for (int i = 0; i < kPeriod; ++i)
-        offset[i] = (key - wave * kRows) * static_cast<uint32_t>(plane.place_stride * 2) + piece_of<kDim>(i * kStep + key, piece) * 16;
+      for (int i = 0; i < kPeriod; ++i) offset[i] = in * static_cast<uint32_t>(plane.place_stride * kSize) + offset_in_row(i);
+      const uint32_t exp_offset = kFp8 ? in * static_cast<uint32_t>(plane.exp_place_stride) : 0;
       const char *from = nullptr;
+      const uint8_t *e = nullptr;
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
         const int row0 = i * kStep + wave * kRows;
         if (i == 0 || p.page_shift < 6) {
           const int64_t page = __builtin_amdgcn_readlane(pages_ahead, 4 * next_block + row0 / 16), place = (k0 + row0) & (p.cache.page - 1);
-          from = rows + (page * plane.page_stride + place * plane.place_stride) * 2;
+          from = rows + (page * plane.page_stride + place * plane.place_stride) * kSize;
+          if constexpr (kFp8) e = exps + (page * plane.exp_page_stride + place * plane.exp_place_stride);
         } else {
-          from += kStep * 2 * plane.place_stride;
+          from += kStep * kSize * plane.place_stride;
+          if constexpr (kFp8) e += kStep * plane.exp_place_stride;
         }
-        load_to_lds(from + offset[i % kPeriod], lds + row0 * kRowBytes);
+        fetch(i, from + offset[i % kPeriod], e + exp_offset, lds);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < kMine; ++i) {
-        int page, place;
-        locate(p, table, k0, to, i, page, place);
-        if constexpr (kFp8) {
-          load_codes(page, place, i);
-        } else {
-          const int row0 = i * kStep + wave * kRows;
-          load_to_lds(rows + (page * plane.page_stride + place * plane.place_stride) * 2 + piece_of<kDim>(i * kStep + key, piece) * 16, lds + row0 * kRowBytes);
-        }
-      }
+      ++next_block;
     }
-    ++next_block;
+  }
+
+  // Starts on a block of keys.
+  __device__ __forceinline__ void bring(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
+  {
+    if constexpr (!kLate) load(p, table, k0, to, lds);
   }
 
   // The block that was started on is there for the workgroup after the next barrier.
   __device__ __forceinline__ void arrive(const AttentionParams &p, const int32_t *table, int k0, int to, char *lds)
   {
     if constexpr (kFp8) {
-      if constexpr (kLate) look_up(p, table, k0, to);
+      if constexpr (kLate) load(p, table, k0, to, lds);
 #pragma unroll
       for (int i = 0; i < kMine; ++i) {
-        const int row = i * kStep + key;
-        if constexpr (kLate) {
-          int page, place;
-          locate(p, table, k0, to, i, page, place);
-          load_codes(page, place, i);
-        }
         const float scale = exponent_scale(exp[i]);
-        *reinterpret_cast<u32x4 *>(lds + row * kRowBytes + piece_of<kDim>(row, piece) * 16) =
-            u32x4{T::template from_e4m3<false>(codes[i][0], scale), T::template from_e4m3<true>(codes[i][0], scale),
-                  T::template from_e4m3<false>(codes[i][1], scale), T::template from_e4m3<true>(codes[i][1], scale)};
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+          const uint32_t a = codes[i][2 * half], b = codes[i][2 * half + 1];
+          *reinterpret_cast<u32x4 *>(lds + (widened_at ^ 16 * half) + i * kStep * kRowBytes) =
+              u32x4{T::template from_e4m3<false>(a, scale), T::template from_e4m3<true>(a, scale), T::template from_e4m3<false>(b, scale), T::template from_e4m3<true>(b, scale)};
+        }
       }
-      if constexpr (kLate) ++next_block;
     } else {
       wait_for_lds_loads();
     }
@@ -143,14 +133,14 @@ struct Loader {
 
   // Rows of the block at k0 that nobody sees (keys outside [from, to)) become zeros. Returns whether any of the others that this thread looks at
   // holds no number.
-  __device__ __forceinline__ int clear(char *lds, int k0, int from, int to) const
+  static __device__ __forceinline__ int clear(char *lds, int k0, int from, int to)
   {
     bool strange = false;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int row = i * kStep + key;
-      u32x4 *at = reinterpret_cast<u32x4 *>(lds + row * kRowBytes + piece * 16);
-      if (k0 + row < from || k0 + row >= to) {
+    for (int i = threadIdx.x; i < ChunkShape::kKeys * kRowBytes / 16; i += kThreads) {
+      const int key = k0 + i / (kRowBytes / 16);
+      u32x4 *at = reinterpret_cast<u32x4 *>(lds) + i;
+      if (key < from || key >= to) {
         *at = u32x4{0, 0, 0, 0};
       } else {
         const u32x4 v = *at;
@@ -220,7 +210,7 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
 
     // Operands from shared memory, asked for kAhead products before they are due. What a product and the work beside it need stays together
     // (sched_barrier): left to itself the compiler reads far ahead and runs out of registers.
-    constexpr int kAhead = 4, kScoreProducts = 2 * kFrags, kValueProducts = 4 * kTiles, kBuffer = kKeys * kRowBytes;
+    constexpr int kAhead = kFp8 ? 3 : 4, kScoreProducts = 2 * kFrags, kValueProducts = 4 * kTiles, kBuffer = kKeys * kRowBytes;
     // The order of pieces is an exclusive or, so the places of a lane's pieces are one number and constants; another bit says which of two
     // buffers. The numbers are made anew for every block (by an empty asm): kept, the places of all pieces would fill thirty registers.
     int key_at = n * kRowBytes + piece_of<kDim>(n, h) * 16, value_at;
