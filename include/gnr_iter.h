@@ -28,6 +28,7 @@ extern "C" {
 #endif
 
 #define ITER_MAX_REQUESTS 1024  /* requests of one batch */
+#define ITER_MAX_TOKENS (1 << 21) /* its tokens; its rows (tokens times query heads of a kv head): 16 times as many */
 #define ITER_MAX_ADAPTERS 2048  /* adapters loaded */
 #define ITER_MAX_RANK 128
 
@@ -79,7 +80,7 @@ int iter_kv_read(const iter_cache *cache, int type, const iter_rows *k, const it
                  int64_t tokens, void *hip_stream);
 
 /* A batch: request r brings the tokens q_start[r] .. q_start[r+1]-1 (one for a decode, a chunk for a prefill, none is
- * fine), which are the last ones of the kv_len[r] that its cache holds; token j of a request lies at place j % page of
+ * fine; a batch of tokens has a request), which are the last ones of the kv_len[r] that its cache holds; token j of a request lies at place j % page of
  * page page_table[r*table_stride + j / page]. All arrays on the device, q_start with requests + 1 entries ascending from 0 to `tokens`.
  * max_q is what the host expects of the longest chunk: it selects kernels, results do not depend on it being right. */
 typedef struct {
@@ -97,7 +98,8 @@ int iter_attention_bytes(const iter_cache *cache, const iter_batch *batch, int h
  * h / (heads / kv_heads). The token at position p = kv_len - q_len + i of its request sees positions max(0, p - window + 1) .. p
  * (window = 0: 0 .. p): out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q.k_j). A token that sees nothing gets zeros. What lies
  * where a token does not look (NaN included) does not matter. Scores, sums and outputs are held in 32 bits; the weights are rounded to `type` for
- * the matrix product with the values, relative to the largest of their row. Rows of tokens outside every request are not written. out must not overlap q. */
+ * the matrix product with the values, relative to the largest of their row. Rows of tokens outside every request (of a batch with
+ * bounds out of range) are not written. out must not overlap q, nor be the same rows. There is no backward pass. */
 int iter_attention(const iter_cache *cache, const iter_batch *batch, int type, int heads, const iter_rows *q,
                    const iter_rows *out, double scale, int64_t window, void *workspace, size_t bytes, uint32_t *status,
                    void *hip_stream);

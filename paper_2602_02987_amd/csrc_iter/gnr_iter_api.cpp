@@ -67,8 +67,9 @@ int check_kv(const iter_cache *c, int type, const iter_rows *k, const iter_rows 
 int check_batch(const iter_cache *c, const iter_batch *b, int heads)
 {
   if (!cache_ok(c) || !b || heads < 1 || heads > kMaxHeads || heads % c->kv_heads != 0) return SIM_EINVAL;
-  if (b->requests < 0 || b->requests > ITER_MAX_REQUESTS || b->tokens < 0 || b->tokens > kMaxTokens) return SIM_EINVAL;
-  if (b->tokens * (heads / c->kv_heads) > kMaxTokens || b->max_q < 0) return SIM_EINVAL;
+  // (numbers of tiles fit 32 bits whatever the device finds in q_start, where every second request may claim all tokens)
+  if (b->requests < 0 || b->requests > ITER_MAX_REQUESTS || b->tokens < 0 || b->tokens > ITER_MAX_TOKENS) return SIM_EINVAL;
+  if (b->tokens * (heads / c->kv_heads) > 16 * int64_t(ITER_MAX_TOKENS) || b->max_q < 0 || (b->tokens > 0 && b->requests == 0)) return SIM_EINVAL;
   if (b->table_stride < 0 || b->table_stride > kMaxStride || b->table_width < 0 || b->table_width > INT32_MAX) return SIM_EINVAL;
   return SIM_OK;
 }
@@ -109,7 +110,8 @@ int iter_attention(const iter_cache *c, const iter_batch *b, int type, int heads
   if (rc != SIM_OK) return rc;
   if (!type_fits(*c, type) || !rows_ok(q, b->tokens) || !rows_ok(out, b->tokens)) return SIM_EINVAL;
   if (!std::isfinite(scale) || window < 0) return SIM_EINVAL;
-  if (b->tokens == 0 || b->requests == 0) return SIM_OK;
+  if (b->tokens == 0) return SIM_OK;
+  if (q->data == out->data) return SIM_EINVAL;
   if (!b->q_start || !b->kv_len || (!b->page_table && b->table_width > 0)) return SIM_EINVAL;
   const size_t need = attention_bytes(*c, *b, heads);
   if (need > 0 && (!workspace || !aligned(workspace))) return SIM_EINVAL;
@@ -129,7 +131,7 @@ int iter_attention(const iter_cache *c, const iter_batch *b, int type, int heads
 
 int iter_adapters_bytes(const iter_adapter_set *s, int64_t tokens, size_t *out_bytes)
 {
-  if (!s || !out_bytes || tokens < 0 || tokens > kMaxTokens || s->rank < 8 || s->rank > ITER_MAX_RANK || s->rank % 8 != 0) return SIM_EINVAL;
+  if (!s || !out_bytes || tokens < 0 || tokens > ITER_MAX_TOKENS || s->rank < 8 || s->rank > ITER_MAX_RANK || s->rank % 8 != 0) return SIM_EINVAL;
   if (s->width_in < 8 || s->width_in > (1 << 24) || s->adapters < 0 || s->adapters > ITER_MAX_ADAPTERS) return SIM_EINVAL;
   *out_bytes = adapters_bytes(*s, tokens);
   return SIM_OK;
@@ -144,10 +146,10 @@ int iter_adapters(const iter_adapter_set *s, int type, int requests, int64_t tok
   if (rc != SIM_OK) return rc;
   if (type != ITER_BF16 && type != ITER_FP16) return SIM_EINVAL;
   if (s->width_in % 8 != 0 || s->width_out < 8 || s->width_out > (1 << 24) || s->width_out % 8 != 0) return SIM_EINVAL;
-  if (requests < 0 || requests > ITER_MAX_REQUESTS) return SIM_EINVAL;
+  if (requests < 0 || requests > ITER_MAX_REQUESTS || (tokens > 0 && requests == 0)) return SIM_EINVAL;
   if (!strides_ok(2, x_stride, base_stride, out_stride) || !span_ok(tokens, x_stride) || !span_ok(tokens, base_stride) || !span_ok(tokens, out_stride))
     return SIM_EINVAL;
-  if (tokens == 0 || requests == 0) return SIM_OK;
+  if (tokens == 0) return SIM_OK;
   if (!q_start || !adapter || !x || !base || !out || !aligned(x) || !aligned(base) || !aligned(out)) return SIM_EINVAL;
   if (s->adapters > 0 && (!s->down || !s->up || !s->scale || !aligned(s->down) || !aligned(s->up))) return SIM_EINVAL;
   if (need > 0 && (!workspace || !aligned(workspace))) return SIM_EINVAL;

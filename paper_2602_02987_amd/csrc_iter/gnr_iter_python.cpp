@@ -5,10 +5,12 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 
 #include <cmath>
+#include <initializer_list>
 
 #include "gnr_iter.h"
 
@@ -51,6 +53,14 @@ struct On {
   void have(const Tensor *t, const char *name) const { TORCH_CHECK_VALUE(!t || t->device() == device, name, " is on another device"); }
   void *stream() const { return c10::hip::getCurrentHIPStream(device.index()).stream(); }
 };
+
+// Nothing here has a backward pass: better no result than one that gradients do not flow through.
+void no_gradient(std::initializer_list<const Tensor *> tensors)
+{
+  if (!c10::GradMode::is_enabled()) return;
+  for (const Tensor *t : tensors)
+    TORCH_CHECK_VALUE(!t || !t->requires_grad(), "the iteration operators have no backward pass: call them under torch.no_grad() or with detached tensors");
+}
 
 // a dimension of one element has no stride that matters
 int64_t step_of(const Tensor &t, int64_t i) { return t.size(i) > 1 ? t.stride(i) : 0; }
@@ -137,6 +147,7 @@ PyObject *kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
   HANDLE_TH_ERRORS
   want(n, 7);
   const Tensor &k = *tensor(a[0], "k"), &v = *tensor(a[1], "v"), &kc = *tensor(a[2], "k_cache"), &vc = *tensor(a[3], "v_cache"), &slots = *tensor(a[4], "slots");
+  no_gradient({&k, &v, &kc, &vc});
   const On on(kc);
   const iter_cache c = cache(kc, vc, optional(a[5], "k_exp"), optional(a[6], "v_exp"), on);
   TORCH_CHECK_VALUE(is_half(k.scalar_type()) && (c.type == ITER_FP8 || k.scalar_type() == kc.scalar_type()),
@@ -156,6 +167,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
   HANDLE_TH_ERRORS
   want(n, 8);
   const Tensor &kc = *tensor(a[0], "k_cache"), &vc = *tensor(a[1], "v_cache"), &slots = *tensor(a[2], "slots");
+  no_gradient({&kc, &vc});
   const On on(kc);
   const iter_cache c = cache(kc, vc, optional(a[3], "k_exp"), optional(a[4], "v_exp"), on);
   const int64_t wanted = integer(a[5], "dtype");
@@ -179,6 +191,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
   want(n, 14);
   const Tensor &q = *tensor(a[0], "q"), &kc = *tensor(a[1], "k_cache"), &vc = *tensor(a[2], "v_cache"), &table = *tensor(a[3], "page_table");
   const Tensor &start = *tensor(a[4], "q_start"), &length = *tensor(a[5], "kv_len");
+  no_gradient({&q, &kc, &vc});
   const On on(q);
   const iter_cache c = cache(kc, vc, optional(a[6], "k_exp"), optional(a[7], "v_exp"), on);
   const at::ScalarType type = q.scalar_type();
@@ -189,7 +202,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
                     "page_table has to be int32 [requests, width] with dense rows");
   on.have(&table, "page_table");
   const Tensor *given = optional(a[11], "out");
-  const Tensor out = given ? *given : at::empty({tokens, heads, c.head_dim}, q.options().requires_grad(false));
+  const Tensor out = given ? *given : at::empty({tokens, heads, c.head_dim}, q.options());
   const iter_rows qr = rows(q, tokens, heads, c.head_dim, type, "q", on), outr = rows(out, tokens, heads, c.head_dim, type, "out", on);
   const int64_t max_q = integer(a[8], "max_q"), window = integer(a[10], "window");
   double scale = 1.0 / std::sqrt(static_cast<double>(c.head_dim));
@@ -219,6 +232,7 @@ PyObject *adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
   const Tensor &x = *tensor(a[0], "x"), &base = *tensor(a[1], "base"), &down = *tensor(a[2], "down"), &up = *tensor(a[3], "up"), &scale = *tensor(a[4], "scale");
   const Tensor &start = *tensor(a[5], "q_start"), &which = *tensor(a[6], "adapter");
   TORCH_CHECK_VALUE(x.dim() == 2 && down.dim() == 3 && up.dim() == 3 && which.dim() == 1, "x has two dimensions, down and up three, adapter one");
+  no_gradient({&x, &base, &down, &up, &scale});
   const On on(x);
   const at::ScalarType type = x.scalar_type();
   const int64_t tokens = x.size(0), wi = x.size(1), count = down.size(0), rank = down.size(1), wo = up.size(1), requests = which.size(0);
@@ -227,7 +241,7 @@ PyObject *adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
                     "down has to be [adapters, rank, width_in] and up [adapters, width_out, rank], without gaps");
   on.have(&base, "base"); on.have(&down, "down"); on.have(&up, "up");
   const Tensor *given = optional(a[7], "out");
-  const Tensor out = given ? *given : at::empty({tokens, wo}, x.options().requires_grad(false));
+  const Tensor out = given ? *given : at::empty({tokens, wo}, x.options());
   on.have(&out, "out");
   TORCH_CHECK_VALUE(base.dim() == 2 && base.size(0) == tokens && base.size(1) == wo && out.dim() == 2 && out.size(0) == tokens && out.size(1) == wo && out.scalar_type() == type,
                     "base and out have to be [", tokens, ", ", wo, "] of ", type);

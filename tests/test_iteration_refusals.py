@@ -101,7 +101,7 @@ def test_cache_calls_that_are_refused():
 
 def _attend(cache=None, batch=None, typ=0, heads=4, q=None, out=None, scale=1.0, window=0, work=P, size=1 << 40):
     c, b = cache or _cache(), batch or _batch()
-    return I._lib().iter_attention(C.byref(c), C.byref(b), typ, heads, C.byref(q or _rows()), C.byref(out or _rows()), scale, window, work, size,
+    return I._lib().iter_attention(C.byref(c), C.byref(b), typ, heads, C.byref(q or _rows()), C.byref(out or _rows(2 * P)), scale, window, work, size,
                                    None, None)
 
 
@@ -123,7 +123,11 @@ def test_attention_calls_that_are_refused():
     assert L.iter_attention_bytes(C.byref(_cache()), C.byref(_batch()), 4, C.byref(need)) == 0
     if need.value:
         assert _attend(work=None) == EINVAL and _attend(work=P + 4) == EINVAL and _attend(size=need.value - 1) == ENOMEM
-    assert _attend(batch=_batch(tokens=0)) == 0 and _attend(batch=_batch(requests=0)) == 0   # nothing to do
+    assert _attend(batch=_batch(tokens=0)) == 0 and _attend(batch=_batch(tokens=0, requests=0)) == 0   # nothing to do
+    assert _attend(batch=_batch(requests=0)) == EINVAL                  # tokens of nobody
+    assert _attend(out=_rows()) == EINVAL                               # over the queries
+    limit = 1 << 21
+    assert _attend(batch=_batch(tokens=limit + 1)) == EINVAL and _attend(_cache(kv_heads=1), _batch(tokens=limit), heads=17) == EINVAL
 
 
 def _adapt(typ=0, requests=2, tokens=5, q_start=P, adapter=P, x=P, xs=64, base=P, bs=128, out=P, os_=128, work=P, size=1 << 40, **kw):
@@ -144,7 +148,8 @@ def test_adapter_calls_that_are_refused():
     assert I._lib().iter_adapters_bytes(C.byref(s), 5, C.byref(need)) == 0
     if need.value:
         assert _adapt(work=None) == EINVAL and _adapt(size=need.value - 1) == ENOMEM
-    assert _adapt(tokens=0) == 0 and _adapt(requests=0) == 0
+    assert _adapt(tokens=0) == 0 and _adapt(tokens=0, requests=0) == 0
+    assert _adapt(requests=0) == EINVAL and _adapt(tokens=(1 << 21) + 1) == EINVAL
 
 
 def test_the_binding_refuses_what_does_not_fit():
@@ -170,6 +175,20 @@ def test_the_binding_refuses_what_does_not_fit():
     for call in (lambda: I.adapters(y, y, d, u, torch.ones(2), i, i[:1]), lambda: I.adapters(y, y.half(), d, u, torch.ones(2), i, i[:1]),
                  lambda: I.adapters(y, y, d, u.transpose(1, 2), torch.ones(2), i, i[:1]), lambda: I.adapters(y, y[:2], d, u, torch.ones(2), i, i[:1])):
         with pytest.raises(ValueError):
+            call()
+
+
+def test_tensors_that_require_gradients_are_refused():
+    k, v, _, _ = I.new_cache(4, 2, 16, 64, device="cpu")
+    i, slots = torch.zeros(2, dtype=torch.int32), torch.zeros(3, dtype=torch.int64)
+    x = torch.zeros(3, 2, 64, dtype=torch.bfloat16, requires_grad=True)
+    y, up = torch.zeros(3, 64, dtype=torch.bfloat16), torch.zeros(2, 64, 8, dtype=torch.bfloat16)
+    down = torch.zeros(2, 8, 64, dtype=torch.bfloat16, requires_grad=True)
+    for call in (lambda: I.kv_write(x, x, k, v, slots), lambda: I.attention(x, k, v, i.view(1, 2), i, i[:1]),
+                 lambda: I.adapters(y, y, down, up, torch.ones(2), i, i[:1])):
+        with pytest.raises(ValueError, match="backward"):
+            call()
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):   # (the next thing that is wrong)
             call()
 
 
