@@ -92,7 +92,7 @@ __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const Adapt
   extern __shared__ int numbers[];
   __shared__ int tokens[kTile];
   __shared__ float sums[kWaves][kRankTiles * 16][17];
-  const int which = find_tile<kTile>(p, blockIdx.x, false, numbers, tokens);
+  const int which = find_tile<kTile>(p, blockIdx.y, false, numbers, tokens);
   if (which < 0) return;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = lane % 16, g = lane / 16;
   const int rank = p.set.rank, width = static_cast<int>(p.set.width_in);
@@ -100,14 +100,14 @@ __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const Adapt
 #pragma unroll
   for (int s = 0; s < kSub; ++s) x[s] = static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(max(tokens[16 * s + n], 0)) * p.x_stride;   // (what is beyond the tile's last is not kept)
   const uint16_t *down = static_cast<const uint16_t *>(p.set.down) + static_cast<int64_t>(which) * rank * width;
-  const int blocks = (width + kDepth - 1) / kDepth, each = (blocks + gridDim.y - 1) / gridDim.y;
-  const int end = min(blocks, static_cast<int>(blockIdx.y + 1) * each);
+  const int blocks = (width + kDepth - 1) / kDepth, each = (blocks + gridDim.x - 1) / gridDim.x;
+  const int end = min(blocks, static_cast<int>(blockIdx.x + 1) * each);
   f32x4 acc[kSub][kRankTiles];
 #pragma unroll
   for (int s = 0; s < kSub; ++s)
 #pragma unroll
     for (int i = 0; i < kRankTiles; ++i) acc[s][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  for (int block = blockIdx.y * each + wave; block < end; block += kWaves) {
+  for (int block = blockIdx.x * each + wave; block < end; block += kWaves) {
     u32x4 a[2][kRankTiles], b[2][kSub];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
@@ -145,7 +145,7 @@ __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const Adapt
       float h = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) h += sums[w][r][t];
-      p.workspace[(static_cast<int64_t>(blockIdx.y) * p.tokens + token) * rank + r] = h;
+      p.workspace[(static_cast<int64_t>(blockIdx.x) * p.tokens + token) * rank + r] = h;
     }
   }
 }
@@ -163,21 +163,24 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
   extern __shared__ int numbers[];
   __shared__ int tokens[kTile];
   __shared__ __attribute__((aligned(16))) float h[kTile][kPitch];
-  const int which = find_tile<kTile>(p, blockIdx.x, true, numbers, tokens);
+  const int which = find_tile<kTile>(p, blockIdx.y, true, numbers, tokens);
   if (which < 0) return;
   const bool none = which == p.set.adapters;
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = lane % 16, g = lane / 16;
   const int rank = p.set.rank, width = static_cast<int>(p.set.width_out);
-  const int column0 = (blockIdx.y * kWaves + wave) * kColumns, column = column0 + 8 * g;   // (and 32 on for the next load)
-  u32x4 y[kLoads];
-  const auto load_base = [&](int s) {
+  const int column0 = (blockIdx.x * kWaves + wave) * kColumns, column = column0 + 8 * g;   // (and 32 on for the next load)
+  // base of all of the tile's tokens where there is room in registers (whole prompt 81 -> 77 us), else of sixteen at a time
+  constexpr int kBuffers = kRankSteps == 1 ? kSub : 1;
+  u32x4 y[kBuffers][kLoads];
+  const auto load_base = [&](int s) GNR_INLINE {
     const int token = tokens[16 * s + n];
     const uint16_t *base = static_cast<const uint16_t *>(p.base) + static_cast<int64_t>(max(token, 0)) * p.base_stride;
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
-      if (column + 32 * j < width) y[j] = *reinterpret_cast<const u32x4 *>(base + column + 32 * j);
+      if (column + 32 * j < width) y[s % kBuffers][j] = *reinterpret_cast<const u32x4 *>(base + column + 32 * j);
   };
-  load_base(0);
+#pragma unroll
+  for (int s = 0; s < kBuffers; ++s) load_base(s);
   u32x4 rows[kRankSteps][kProducts];
   float by = 0.0f;
   if (!none) {
@@ -252,7 +255,7 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
     u32x4 z[kLoads];
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
-      z[j] = y[j];
+      z[j] = y[s % kBuffers][j];
       if (!none) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
@@ -261,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
         }
       }
     }
-    if (s + 1 < kSub) load_base(s + 1);
+    if (s + kBuffers < kSub) load_base(s + kBuffers);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
       if (token >= 0 && column + 32 * j < width) *reinterpret_cast<u32x4 *>(out + column + 32 * j) = z[j];
@@ -296,8 +299,10 @@ static int launch(const AdapterParams &p, hipStream_t s)
 {
   const size_t lds = static_cast<size_t>(p.set.adapters + 1 + 2 * p.requests) * sizeof(int);
   const int splits = splits_for(p.set, p.tokens);
-  const dim3 down(static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, false)), static_cast<unsigned>(splits));
-  const dim3 up(static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, true)), static_cast<unsigned>((p.set.width_out + kColumns * kWaves - 1) / (kColumns * kWaves)));
+  // the workgroups of a tile run beside each other, so that whole rows of x, base and out are read and written at a time (whole prompt 87 -> 81 us,
+  // mixed iteration 20.2 -> 17.8)
+  const dim3 down(static_cast<unsigned>(splits), static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, false)));
+  const dim3 up(static_cast<unsigned>((p.set.width_out + kColumns * kWaves - 1) / (kColumns * kWaves)), static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, true)));
   if (p.set.adapters > 0) {
     if (p.set.rank <= 16) gnr_adapters_down_kernel<T, 1, kSub><<<down, kThreads, lds, s>>>(p);
     else if (p.set.rank <= 32) gnr_adapters_down_kernel<T, 2, kSub><<<down, kThreads, lds, s>>>(p);
