@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
       }
       return keep;
     };
-    const auto weigh = [&](u32x4 (&to_weights)[4], auto i) GNR_INLINE {   // scores 2 i and 2 i + 1
+    const auto weigh = [&](auto i) GNR_INLINE {                 // scores 2 i and 2 i + 1
       constexpr int j = 2 * (i % 8), word = i % 4;
       const f32x16 &x = i < 8 ? low : high;
       const float a = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j], p.scale_log2, -top)), b = __builtin_amdgcn_exp2f(__builtin_fmaf(x[j + 1], p.scale_log2, -top));
@@ -274,18 +274,22 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
       sum += b;
       uint32_t both = T::narrow2(a, b);
       asm volatile("" : "+v"(both));                            // (stays where it is: the compiler would move it all behind the products)
-      to_weights[i / 4][word] = both;
+      w[i / 4][word] = both;
     };
-    // The weights' products with their values and, beside them, the weights of the block after, whose scores are there already.
-    const auto add = [&](auto also, u32x4 (&next)[4]) GNR_INLINE {
-      constexpr int kEach = kValueProducts < 16 ? 16 / kValueProducts : 1;
+    // The weights' products with their values and, beside them, the weights of the block after, whose scores are there already. They take the places of
+    // weights that have been multiplied, so the sixteen words are spread from the last product of the first four words on: as many by the end of product n as
+    // due(n). (A second set of words and its copies: whole prompt 571 -> 568 us, long prompt's chunk 163.5 -> 161.5 without.)
+    constexpr auto due = [](int products) {
+      const int free = products / kTiles * 4, of = kValueProducts - kTiles + 1, n = products - kTiles + 1, share = n <= 0 ? 0 : (n * 16 + of - 1) / of;
+      return share < free ? share : free;
+    };
+    const auto add = [&](auto also) GNR_INLINE {
       u32x4 operand[kAhead];
       repeat<kAhead>([&](auto i) GNR_INLINE { operand[i] = value_operand(i); });
       repeat<kValueProducts>([&](auto i) GNR_INLINE {
         acc[i % kTiles] = T::mfma32(bits<oct>(operand[i % kAhead]), bits<oct>(w[i / kTiles]), acc[i % kTiles]);
         if constexpr (i + kAhead < kValueProducts) operand[i % kAhead] = value_operand(std::integral_constant<int, i + kAhead>{});
-        if constexpr (also && (kValueProducts <= 16 || i % 2 == 0))
-          repeat<kEach>([&](auto k) GNR_INLINE { weigh(next, std::integral_constant<int, 16 * i / kValueProducts + k>{}); });
+        if constexpr (also) repeat<due(i + 1) - due(i)>([&](auto k) GNR_INLINE { weigh(std::integral_constant<int, due(i) + k>{}); });
         __builtin_amdgcn_sched_barrier(0);
       });
     };
@@ -303,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
       if (from + kKeys < to) key_loader.bring(p, table, from + kKeys, to, keys + kBuffer);
       score();
       settle(from);
-      repeat<16>([&](auto i) GNR_INLINE { weigh(w, i); });
+      repeat<16>([&](auto i) GNR_INLINE { weigh(i); });
       // A weight of zero does not silence a NaN or an infinity: where any stands among values that not every row sees, the rows are
       // computed again by the kernel that joins.
       const auto check_values = [&](int k0) GNR_INLINE {
@@ -324,19 +328,22 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
         check_values(k0);
         value_loader.bring(p, table, k0 + kKeys, to, values + (buffer ^ kBuffer));
         if (k0 + 2 * kKeys < to) key_loader.bring(p, table, k0 + 2 * kKeys, to, keys + buffer);
+        // (of a SIMD's two waves the one whose products are due goes first: long prompt's chunk 173 -> 164 us, whole prompt 596 -> 590)
+        __builtin_amdgcn_s_setprio(1);
         score();
+        __builtin_amdgcn_s_setprio(0);
         const float keep = settle(k0 + kKeys);
-        u32x4 next[4];
-        add(std::true_type{}, next);
+        __builtin_amdgcn_s_setprio(2);
+        add(std::true_type{});
+        __builtin_amdgcn_s_setprio(0);
         if (__any(keep != 1.0f)) repeat<kTiles>([&](auto e) GNR_INLINE { acc[e] *= keep; });
-        repeat<4>([&](auto i) GNR_INLINE { w[i] = next[i]; });
         value_at ^= kBuffer;
         buffer ^= kBuffer;
       }
       value_loader.arrive(p, table, k0, to, values + buffer);
       __syncthreads();
       check_values(k0);
-      add(std::false_type{}, w);
+      add(std::false_type{});
     }
     again = __syncthreads_or(again);                            // (and nobody reads the last block any more)
     if (threadIdx.x == 0) mark(p, ChunkShape::kPlan, u, again);
