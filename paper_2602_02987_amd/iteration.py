@@ -22,7 +22,10 @@ import torch
 from .binding import SimError, lib
 
 lib()                          # (torch first, then the library, then what links against both)
-from . import _iteration       # noqa: E402
+try:
+    from . import _iteration   # noqa: E402
+except ImportError as e:
+    raise ImportError("the compiled binding is missing or does not fit this torch: run `python -m paper_2602_02987_amd.build`") from e
 
 SIM_EINVAL = -1
 BAD_BATCH, BAD_PAGE, BAD_ADAPTER = 1, 2, 4

@@ -427,6 +427,37 @@ def test_cache_write_and_read(dim, kind, qt, tokens, heads, places, tm):
         assert np.array_equal(values[pg, :, pl], before[i][pg, :, pl])     # nothing else is touched
 
 
+@pytest.mark.parametrize("dim,heads,places", [(64, 8, 16), (128, 4, 64), (256, 12, 32)])
+@pytest.mark.parametrize("kind,qt", [("bf16", "bf16"), ("fp8", "fp16")])
+def test_many_rows_as_in_small_calls(dim, heads, places, kind, qt):
+    """Calls of more rows take several heads a workgroup; the same bits as in calls of a few tokens, which are held to 64 bits above. Some slots are no
+    place, results go to parts of larger tensors."""
+    gen = _gen(dim)
+    tokens = -(-33000 // heads) + 3
+    pages = -(-tokens // places) + 1
+    new = (torch.randn((tokens, 2, heads, dim), generator=gen) * torch.exp(2 * torch.randn((tokens, 2, heads, 1), generator=gen))).to(R.TYPES[qt]).to(DEV)
+    new[5, 0, 1, 3], new[6, 1, 2, 4] = float("nan"), float("inf")
+    slots = torch.randperm(pages * places, generator=gen)[:tokens].to(DEV)
+    slots[torch.randperm(tokens, generator=gen)[:7].to(DEV)] = -1
+    caches = [I.new_cache(pages, heads, places, dim, R.TYPES[kind], DEV) for _ in range(2)]
+    for (k, v, ke, ve), step in zip(caches, (tokens, 500)):
+        for t in range(0, tokens, step):
+            I.kv_write(new[t:t + step, 0], new[t:t + step, 1], k, v, slots[t:t + step], ke, ve)
+    for a, b in zip(*caches):
+        assert a is None or torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    k, v, ke, ve = caches[0]
+    room = torch.full((tokens, 2, heads + 1, dim + 8), 5.0, dtype=R.TYPES[qt], device=DEV)
+    rk, rv = room[:, 0, :heads, :dim], room[:, 1, 1:, 8:]
+    I.kv_read(k, v, slots, ke, ve, dtype=R.TYPES[qt], k=rk, v=rv)
+    for t in range(0, tokens, 500):
+        sk, sv = I.kv_read(k, v, slots[t:t + 500], ke, ve, dtype=R.TYPES[qt])
+        for got, want in ((rk[t:t + 500], sk), (rv[t:t + 500], sv)):
+            assert torch.equal(got.contiguous().view(torch.int16), want.view(torch.int16))
+    rk.fill_(5.0)
+    rv.fill_(5.0)
+    assert (room == 5.0).all()
+
+
 @pytest.mark.parametrize("qt", ["bf16", "fp16"])
 def test_quantising_every_kind_of_row(qt):
     """Rows at the borders: powers of two, 448 times them and the next value above, subnormal numbers, the largest ones, ties,
@@ -490,6 +521,7 @@ ADAPTERS = [
     ("fp16", 8, 8000, 8, 2, [5, 1], [-1, -1]),
     ("bf16", 40, 264, 520, 3, [1] * 30 + [2100], [i % 4 - 1 for i in range(30)] + [2]),     # many tokens: larger tiles
     ("fp16", 128, 1032, 776, 2, [1000, 1, 1500, 3], [1, 0, -1, 1]),
+    ("bf16", 32, 512, 1160, 3, [1] * 5 + [2070, 3], [2, -1, 0, 1, 1, 2, 0]),
 ]
 
 
