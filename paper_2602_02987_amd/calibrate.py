@@ -5,7 +5,8 @@ c0 + c_pre * prefill_tokens + c_dec * n_decode to them; what it prints can be ha
 
 `Server` is the block itself: a paged cache (8-bit or as the activations), projections that all requests share (plain matrix products of the
 library), an adapter for each class beside them, and attention of all tokens of an iteration over their requests' caches. A request can be
-moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time.
+moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time. A model's feed-forward blocks are not
+in these times.
 """
 from __future__ import annotations
 
