@@ -35,21 +35,21 @@ __device__ __forceinline__ int wave_scan(int v)   // of the lanes up to this one
 // Tokens are taken in tiles with the same adapter, in the order of the batch; those without one come last. Every workgroup finds its tile
 // from the batch itself, every wave for itself once the numbers are in shared memory (a barrier costs more). Returns the adapter, or
 // -1 when there are fewer tiles; tokens[i] is -1 beyond the tile's last. numbers: shared, adapters + 1 and two for each request.
-template <int kTile>
+template <int kTile, int kCount = kThreads>
 __device__ __forceinline__ int find_tile(const AdapterParams &p, int tile, bool with_none, int *numbers, int *tokens)
 {
   const int all = p.set.adapters + 1, n = p.requests, lane = threadIdx.x % 64;
   int *counts = numbers, *lens = numbers + all, *whose = lens + n;
   uint32_t flags = 0;
-  for (int a = threadIdx.x; a < all; a += kThreads) counts[a] = 0;
-  for (int r = threadIdx.x; r < n; r += kThreads) {
+  for (int a = threadIdx.x; a < all; a += kCount) counts[a] = 0;
+  for (int r = threadIdx.x; r < n; r += kCount) {
     int which;
     lens[r] = tokens_of(p, r, which, flags);
     whose[r] = which;
   }
   if (threadIdx.x < kTile) tokens[threadIdx.x] = -1;
   __syncthreads();
-  for (int r = threadIdx.x; r < n; r += kThreads)
+  for (int r = threadIdx.x; r < n; r += kCount)
     if (lens[r]) atomicAdd(&counts[whose[r]], lens[r]);   // (whole numbers: the order does not matter)
   if (flags && p.status && blockIdx.x == 0 && blockIdx.y == 0) atomicOr(p.status, flags);
   __syncthreads();
@@ -151,40 +151,22 @@ __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const Adapt
   }
 }
 
-// out = base + scale up h of a tile, 128 columns to a wave: Y^T = up H^T with 16 rows of up at a time as the left operand. h is in 32 bits; it goes
+// up h of 16 tokens for kCols columns of a wave: Y^T = up H^T with 16 rows of up at a time as the left operand. h is in 32 bits; it goes
 // into the product as the sum of two 16-bit numbers, relative to a power of two near the token's largest, so that neither type's range nor
 // its precision shows. The rows of up that two products take are chosen so that a lane ends up with eight neighbouring columns of its token, and the four
-// lanes of a token with 32: base and out are read and written 16 bytes a lane, 64 a token. Bound by these two; for few tokens by latency, so base and the rows of up are asked for
-// before h is added up. 8191 tokens, width 6144, rank 32: 52 us (3.9 TB/s); 128 tokens: 7 us.
-template <class T, int kRankSteps, int kSub>
-__global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapters_up_kernel(const AdapterParams p, int splits)
-{
+// lanes of a token with 32: base and out are read and written 16 bytes a lane, 64 a token.
+template <class T, int kRankSteps, int kCols>
+struct Columns {
   typedef typename T::oct oct;
-  constexpr int kTile = 16 * kSub, kProducts = kColumns / 16, kLoads = kColumns / 32, kPitch = kRankSteps * 32 + 4;
-  extern __shared__ int numbers[];
-  __shared__ int tokens[kTile];
-  __shared__ __attribute__((aligned(16))) float h[kTile][kPitch];
-  const int which = find_tile<kTile>(p, blockIdx.y, true, numbers, tokens);
-  if (which < 0) return;
-  const bool none = which == p.set.adapters;
-  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, n = lane % 16, g = lane / 16;
-  const int rank = p.set.rank, width = static_cast<int>(p.set.width_out);
-  const int column0 = (blockIdx.x * kWaves + wave) * kColumns, column = column0 + 8 * g;   // (and 32 on for the next load)
-  // base of all of the tile's tokens where there is room in registers (whole prompt 81 -> 77 us), else of sixteen at a time
-  constexpr int kBuffers = kRankSteps == 1 ? kSub : 1;
-  u32x4 y[kBuffers][kLoads];
-  const auto load_base = [&](int s) GNR_INLINE {
-    const int token = tokens[16 * s + n];
-    const uint16_t *base = static_cast<const uint16_t *>(p.base) + static_cast<int64_t>(max(token, 0)) * p.base_stride;
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      if (column + 32 * j < width) y[s % kBuffers][j] = *reinterpret_cast<const u32x4 *>(base + column + 32 * j);
-  };
-#pragma unroll
-  for (int s = 0; s < kBuffers; ++s) load_base(s);
+  static constexpr int kProducts = kCols / 16, kLoads = kCols / 32;
+  const int n, g, column0, column, width;                       // column: this lane's first, 32 on for the next load
   u32x4 rows[kRankSteps][kProducts];
-  float by = 0.0f;
-  if (!none) {
+
+  __device__ __forceinline__ Columns(int lane, int first, int all) : n(lane % 16), g(lane / 16), column0(first), column(first + 8 * g), width(all) {}
+
+  __device__ __forceinline__ void load_rows(const AdapterParams &p, int which)
+  {
+    const int rank = p.set.rank;
     const uint16_t *up = static_cast<const uint16_t *>(p.set.up) + static_cast<int64_t>(which) * width * rank;
 #pragma unroll
     for (int i = 0; i < kRankSteps; ++i)
@@ -194,6 +176,99 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
         rows[i][j] = u32x4{0, 0, 0, 0};
         if (row < width && r < rank) rows[i][j] = *reinterpret_cast<const u32x4 *>(up + static_cast<int64_t>(row) * rank + r);
       }
+  }
+
+  __device__ __forceinline__ void load_base(const AdapterParams &p, int token, u32x4 (&y)[kLoads]) const
+  {
+    const uint16_t *base = static_cast<const uint16_t *>(p.base) + static_cast<int64_t>(max(token, 0)) * p.base_stride;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      if (column + 32 * j < width) y[j] = *reinterpret_cast<const u32x4 *>(base + column + 32 * j);
+  }
+
+  // z += by * up h for this lane's token, h (32 kRankSteps numbers) in shared memory
+  __device__ __forceinline__ void add(const float *h, float by, u32x4 (&z)[kLoads]) const
+  {
+    float v[kRankSteps][8], most = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kRankSteps; ++i) {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(h + 32 * i + 8 * g + 4 * k);
+#pragma unroll
+        for (int l = 0; l < 4; ++l) {
+          v[i][4 * k + l] = x[l];
+          most = fmaxf(most, __builtin_fabsf(x[l]));
+        }
+      }
+    }
+    most = fmaxf(most, __shfl_xor(most, 16));
+    most = fmaxf(most, __shfl_xor(most, 32));
+    // 2^-e with most = m 2^e, m in [1, 2); none for what has no such e
+    const uint32_t e = bits<uint32_t>(most) >> 23;
+    const bool plain = e < 1 || e > 253;
+    const float shrink = plain ? 1.0f : bits<float>((254 - e) << 23);
+    const float factor = by * (plain ? 1.0f : bits<float>(e << 23));
+    f32x4 acc[kProducts];
+#pragma unroll
+    for (int j = 0; j < kProducts; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int i = 0; i < kRankSteps; ++i) {
+      u32x4 hi, lo;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float a = v[i][2 * k] * shrink, b = v[i][2 * k + 1] * shrink;
+        hi[k] = T::narrow2(a, b);
+        const float c = a - T::widen(hi[k] & 0xFFFFu), d = b - T::widen(hi[k] >> 16);
+        lo[k] = T::narrow2(c == c ? c : 0.0f, d == d ? d : 0.0f);   // (an infinity is its own upper part)
+      }
+#pragma unroll
+      for (int j = 0; j < kProducts; ++j) {
+        acc[j] = T::mfma16(bits<oct>(rows[i][j]), bits<oct>(hi), acc[j]);
+        acc[j] = T::mfma16(bits<oct>(rows[i][j]), bits<oct>(lo), acc[j]);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const float a = acc[2 * j + k / 2][2 * (k % 2)], b = acc[2 * j + k / 2][2 * (k % 2) + 1];
+        z[j][k] = T::narrow2(__builtin_fmaf(a, factor, T::widen(z[j][k] & 0xFFFFu)), __builtin_fmaf(b, factor, T::widen(z[j][k] >> 16)));
+      }
+  }
+
+  __device__ __forceinline__ void store(const AdapterParams &p, int token, const u32x4 (&z)[kLoads]) const
+  {
+    uint16_t *out = static_cast<uint16_t *>(p.out) + static_cast<int64_t>(max(token, 0)) * p.out_stride;
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      if (token >= 0 && column + 32 * j < width) *reinterpret_cast<u32x4 *>(out + column + 32 * j) = z[j];
+  }
+};
+
+// out = base + scale up h of a tile, 128 columns to a wave. Bound by reading base and writing out; base and the rows of up are asked for
+// before h is added up. 8191 tokens, width 6144, rank 32: 52 us (3.9 TB/s).
+template <class T, int kRankSteps, int kSub>
+__global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapters_up_kernel(const AdapterParams p, int splits)
+{
+  typedef Columns<T, kRankSteps, kColumns> Mine;
+  constexpr int kTile = 16 * kSub, kPitch = kRankSteps * 32 + 4;
+  extern __shared__ int numbers[];
+  __shared__ int tokens[kTile];
+  __shared__ __attribute__((aligned(16))) float h[kTile][kPitch];
+  const int which = find_tile<kTile>(p, blockIdx.y, true, numbers, tokens);
+  if (which < 0) return;
+  const bool none = which == p.set.adapters;
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, rank = p.set.rank;
+  Mine mine(lane, (blockIdx.x * kWaves + wave) * kColumns, static_cast<int>(p.set.width_out));
+  // base of all of the tile's tokens where there is room in registers (whole prompt 81 -> 77 us), else of sixteen at a time
+  constexpr int kBuffers = kRankSteps == 1 ? kSub : 1;
+  u32x4 y[kBuffers][Mine::kLoads];
+#pragma unroll
+  for (int s = 0; s < kBuffers; ++s) mine.load_base(p, tokens[16 * s + mine.n], y[s]);
+  float by = 0.0f;
+  if (!none) {
+    mine.load_rows(p, which);
     by = p.set.scale[which];
     for (int i = threadIdx.x; i < kTile * kRankSteps * 8; i += kThreads) {
       const int t = i / (kRankSteps * 8), r = i % (kRankSteps * 8) * 4, token = tokens[t];
@@ -209,67 +284,84 @@ __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapter
   }
 #pragma unroll
   for (int s = 0; s < kSub; ++s) {
-    const int token = tokens[16 * s + n];
-    f32x4 acc[kProducts];
-    float factor = 0.0f;
-    if (!none) {
-      float v[kRankSteps][8], most = 0.0f;
+    const int token = tokens[16 * s + mine.n];
+    u32x4 z[Mine::kLoads];
 #pragma unroll
-      for (int i = 0; i < kRankSteps; ++i) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-          const f32x4 x = *reinterpret_cast<const f32x4 *>(&h[16 * s + n][32 * i + 8 * g + 4 * k]);
-#pragma unroll
-          for (int l = 0; l < 4; ++l) {
-            v[i][4 * k + l] = x[l];
-            most = fmaxf(most, __builtin_fabsf(x[l]));
-          }
-        }
-      }
-      most = fmaxf(most, __shfl_xor(most, 16));
-      most = fmaxf(most, __shfl_xor(most, 32));
-      // 2^-e with most = m 2^e, m in [1, 2); none for what has no such e
-      const uint32_t e = bits<uint32_t>(most) >> 23;
-      const bool plain = e < 1 || e > 253;
-      const float shrink = plain ? 1.0f : bits<float>((254 - e) << 23);
-      factor = by * (plain ? 1.0f : bits<float>(e << 23));
-#pragma unroll
-      for (int j = 0; j < kProducts; ++j) acc[j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-      for (int i = 0; i < kRankSteps; ++i) {
-        u32x4 hi, lo;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float a = v[i][2 * k] * shrink, b = v[i][2 * k + 1] * shrink;
-          hi[k] = T::narrow2(a, b);
-          const float c = a - T::widen(hi[k] & 0xFFFFu), d = b - T::widen(hi[k] >> 16);
-          lo[k] = T::narrow2(c == c ? c : 0.0f, d == d ? d : 0.0f);   // (an infinity is its own upper part)
-        }
-#pragma unroll
-        for (int j = 0; j < kProducts; ++j) {
-          acc[j] = T::mfma16(bits<oct>(rows[i][j]), bits<oct>(hi), acc[j]);
-          acc[j] = T::mfma16(bits<oct>(rows[i][j]), bits<oct>(lo), acc[j]);
-        }
-      }
-    }
-    uint16_t *out = static_cast<uint16_t *>(p.out) + static_cast<int64_t>(max(token, 0)) * p.out_stride;
-    u32x4 z[kLoads];
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      z[j] = y[s % kBuffers][j];
-      if (!none) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const float a = acc[2 * j + k / 2][2 * (k % 2)], b = acc[2 * j + k / 2][2 * (k % 2) + 1];
-          z[j][k] = T::narrow2(__builtin_fmaf(a, factor, T::widen(z[j][k] & 0xFFFFu)), __builtin_fmaf(b, factor, T::widen(z[j][k] >> 16)));
-        }
-      }
-    }
-    if (s + kBuffers < kSub) load_base(s + kBuffers);
-#pragma unroll
-    for (int j = 0; j < kLoads; ++j)
-      if (token >= 0 && column + 32 * j < width) *reinterpret_cast<u32x4 *>(out + column + 32 * j) = z[j];
+    for (int j = 0; j < Mine::kLoads; ++j) z[j] = y[s % kBuffers][j];
+    if (!none) mine.add(h[16 * s + mine.n], by, z);
+    if (s + kBuffers < kSub) mine.load_base(p, tokens[16 * (s + kBuffers) + mine.n], y[s % kBuffers]);
+    mine.store(p, token, z);
   }
+}
+
+// Both products of a tile of 16 tokens in one launch, for 512 columns: every workgroup multiplies down x by itself, sixteen waves over the elements of x, so that
+// no wave has to wait for memory more than a time or two. For few tokens, which latency bounds: a launch less pays for x and down being read
+// again for every 512 columns (see launch_tiles for where).
+constexpr int kBothWaves = 16, kBothThreads = 64 * kBothWaves, kBothColumns = 32;
+template <class T, int kRankTiles>
+__global__ void __launch_bounds__(kBothThreads) gnr_adapters_both_kernel(const AdapterParams p)
+{
+  typedef typename T::oct oct;
+  constexpr int kRankSteps = (kRankTiles + 1) / 2, kPitch = kRankSteps * 32 + 4;
+  typedef Columns<T, kRankSteps, kBothColumns> Mine;
+  extern __shared__ int numbers[];
+  __shared__ int tokens[16];
+  __shared__ float sums[kBothWaves][kRankTiles * 16][17];
+  __shared__ __attribute__((aligned(16))) float h[16][kPitch];
+  const int which = find_tile<16, kBothThreads>(p, blockIdx.y, true, numbers, tokens);
+  if (which < 0) return;
+  const bool none = which == p.set.adapters;
+  const int lane = threadIdx.x % 64, wave = uniform(static_cast<int>(threadIdx.x / 64)), rank = p.set.rank, width = static_cast<int>(p.set.width_in);
+  Mine mine(lane, (blockIdx.x * kBothWaves + wave) * kBothColumns, static_cast<int>(p.set.width_out));
+  const int n = mine.n, g = mine.g, token = tokens[n];
+  u32x4 y[Mine::kLoads];
+  mine.load_base(p, token, y);
+  if (!none) {
+    mine.load_rows(p, which);
+    const float by = p.set.scale[which];
+    const uint16_t *x = static_cast<const uint16_t *>(p.x) + static_cast<int64_t>(max(token, 0)) * p.x_stride;   // (what is beyond the tile's last is not kept)
+    const uint16_t *down = static_cast<const uint16_t *>(p.set.down) + static_cast<int64_t>(which) * rank * width;
+    f32x4 acc[kRankTiles];
+#pragma unroll
+    for (int i = 0; i < kRankTiles; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    constexpr int kAtOnce = kRankTiles == 4 ? 2 : 4, kElements = 32 * kBothWaves * kAtOnce;   // (by the registers that 1024 threads leave a lane)
+    for (int d0 = 32 * wave; d0 < width; d0 += kElements) {
+      u32x4 a[kAtOnce][kRankTiles], b[kAtOnce];
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int d = d0 + 32 * kBothWaves * u + 8 * g;
+        const bool in = d < width;
+        b[u] = u32x4{0, 0, 0, 0};
+        if (in) b[u] = *reinterpret_cast<const u32x4 *>(x + d);
+#pragma unroll
+        for (int i = 0; i < kRankTiles; ++i) {
+          a[u][i] = u32x4{0, 0, 0, 0};
+          if (in && 16 * i + n < rank) a[u][i] = *reinterpret_cast<const u32x4 *>(down + static_cast<int64_t>(16 * i + n) * width + d);
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u)
+#pragma unroll
+        for (int i = 0; i < kRankTiles; ++i) acc[i] = T::mfma16(bits<oct>(a[u][i]), bits<oct>(b[u]), acc[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < kRankTiles; ++i)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) sums[wave][16 * i + 4 * g + k][n] = acc[i][k];
+    __syncthreads();
+    for (int i = threadIdx.x; i < 16 * 32 * kRankSteps; i += kBothThreads) {
+      const int t = i % 16, r = i / 16;
+      float sum = 0.0f;
+      if (r < rank) {
+#pragma unroll
+        for (int w = 0; w < kBothWaves; ++w) sum += sums[w][r][t];
+      }
+      h[t][r] = sum;
+    }
+    __syncthreads();
+    mine.add(h[n], by, y);
+  }
+  mine.store(p, token, y);
 }
 
 static int tile_tokens(int64_t tokens) { return tokens >= kManyTokens ? 64 : 16; }
@@ -318,10 +410,24 @@ static int launch(const AdapterParams &p, hipStream_t s)
   return iter_hip_ok(hipGetLastError());
 }
 
+// One launch for both products as long as what a workgroup reads of x and down is little, and what all of them do. us by two launches and by one, (tokens, rank, width in,
+// width out): (128, 32, 1024, 1024) 11.7 and 8.4, (700, 32, 512, 512) 18.7 and 10.4, (40, 24, 2000, 8000) 11.2 and 8.4, (1500, 16, 2048, 2048) 25.5 and 20.1; where a workgroup reads more,
+// (128, 16, 4096, 6144) 11.6 and 12.8, (128, 64, 4096, 4096) 15.0 and 25.8; where they all read 91 MB, (1000, 64, 1024, 4096), 29.8 and 34.0.
+constexpr int64_t kBothBytes = 160 << 10, kBothAll = 64 << 20;
 template <class T>
 static int launch_tiles(const AdapterParams &p, hipStream_t s)
 {
-  return tile_tokens(p.tokens) == 64 ? launch<T, 4>(p, s) : launch<T, 1>(p, s);
+  if (tile_tokens(p.tokens) == 64) return launch<T, 4>(p, s);
+  const dim3 both(static_cast<unsigned>((p.set.width_out + kBothColumns * kBothWaves - 1) / (kBothColumns * kBothWaves)), static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, true)));
+  const int64_t bytes = (16 + static_cast<int64_t>(p.set.rank)) * p.set.width_in * 2;
+  if (p.set.rank <= 64 && bytes <= kBothBytes && bytes * both.x * both.y <= kBothAll) {
+    const size_t lds = static_cast<size_t>(p.set.adapters + 1 + 2 * p.requests) * sizeof(int);
+    if (p.set.rank <= 16) gnr_adapters_both_kernel<T, 1><<<both, kBothThreads, lds, s>>>(p);
+    else if (p.set.rank <= 32) gnr_adapters_both_kernel<T, 2><<<both, kBothThreads, lds, s>>>(p);
+    else gnr_adapters_both_kernel<T, 4><<<both, kBothThreads, lds, s>>>(p);
+    return iter_hip_ok(hipGetLastError());
+  }
+  return launch<T, 1>(p, s);
 }
 
 int launch_adapters(const AdapterParams &p, void *stream)

@@ -522,6 +522,9 @@ ADAPTERS = [
     ("bf16", 40, 264, 520, 3, [1] * 30 + [2100], [i % 4 - 1 for i in range(30)] + [2]),     # many tokens: larger tiles
     ("fp16", 128, 1032, 776, 2, [1000, 1, 1500, 3], [1, 0, -1, 1]),
     ("bf16", 32, 512, 1160, 3, [1] * 5 + [2070, 3], [2, -1, 0, 1, 1, 2, 0]),
+    ("fp16", 64, 1024, 1032, 3, [1] * 20 + [70, 0, 3], [i % 4 - 1 for i in range(20)] + [2, 0, -1]),   # both products in one launch
+    ("bf16", 16, 2000, 520, 2, [300, 1, 17], [1, 0, 1]),
+    ("fp16", 32, 8, 1000, 1, [33], [0]),
 ]
 
 
