@@ -106,7 +106,7 @@ int iter_attention(const iter_cache *cache, const iter_batch *batch, int type, i
 
 /* Low-rank adapters, beside a projection that all requests share: for the tokens t of request r with a = adapter[r],
  * out[t] = base[t] + scale[a] * up[a] (down[a] x[t]), out[t] = base[t] for a = -1. x is [tokens][width_in], base and out
- * [tokens][width_out] (rows 16-byte aligned, out may be base itself), down [adapters][rank][width_in] and up
+ * [tokens][width_out] (rows 16-byte aligned; out may be base itself, and either may be or overlap x), down [adapters][rank][width_in] and up
  * [adapters][width_out][rank] without gaps, all of `type`; scale fp32. Widths and rank: multiples of 8, rank up to ITER_MAX_RANK. */
 typedef struct {
   int adapters, rank;

@@ -413,14 +413,26 @@ static int launch(const AdapterParams &p, hipStream_t s)
 // One launch for both products as long as what a workgroup reads of x and down is little, and what all of them do. us by two launches and by one, (tokens, rank, width in,
 // width out): (128, 32, 1024, 1024) 11.7 and 8.4, (700, 32, 512, 512) 18.7 and 10.4, (40, 24, 2000, 8000) 11.2 and 8.4, (1500, 16, 2048, 2048) 25.5 and 20.1; where a workgroup reads more,
 // (128, 16, 4096, 6144) 11.6 and 12.8, (128, 64, 4096, 4096) 15.0 and 25.8; where they all read 91 MB, (1000, 64, 1024, 4096), 29.8 and 34.0.
+// Not where out may overlap x: a workgroup would read rows of x that another of the tile's has written over. (Of two launches the first has read all of x.)
 constexpr int64_t kBothBytes = 160 << 10, kBothAll = 64 << 20;
+static bool may_overlap_x(const AdapterParams &p)
+{
+  const auto first = [](const void *at) { return static_cast<int64_t>(reinterpret_cast<uintptr_t>(at)); };
+  const int64_t x = first(p.x), out = first(p.out), x_row = 2 * p.set.width_in, out_row = 2 * p.set.width_out, step = 2 * p.x_stride;
+  if (out >= x + (p.tokens - 1) * step + x_row || x >= out + (p.tokens - 1) * 2 * p.out_stride + out_row) return false;
+  // rows of one buffer side by side, each with its own columns
+  if (p.x_stride != p.out_stride || step == 0) return true;
+  const int64_t ahead = ((out - x) % step + step) % step;
+  return ahead < x_row || ahead + out_row > step;
+}
+
 template <class T>
 static int launch_tiles(const AdapterParams &p, hipStream_t s)
 {
   if (tile_tokens(p.tokens) == 64) return launch<T, 4>(p, s);
   const dim3 both(static_cast<unsigned>((p.set.width_out + kBothColumns * kBothWaves - 1) / (kBothColumns * kBothWaves)), static_cast<unsigned>(tiles_bound(p.set, p.requests, p.tokens, true)));
   const int64_t bytes = (16 + static_cast<int64_t>(p.set.rank)) * p.set.width_in * 2;
-  if (p.set.rank <= 64 && bytes <= kBothBytes && bytes * both.x * both.y <= kBothAll) {
+  if (p.set.rank <= 64 && bytes <= kBothBytes && bytes * both.x * both.y <= kBothAll && !may_overlap_x(p)) {
     const size_t lds = static_cast<size_t>(p.set.adapters + 1 + 2 * p.requests) * sizeof(int);
     if (p.set.rank <= 16) gnr_adapters_both_kernel<T, 1><<<both, kBothThreads, lds, s>>>(p);
     else if (p.set.rank <= 32) gnr_adapters_both_kernel<T, 2><<<both, kBothThreads, lds, s>>>(p);
