@@ -224,11 +224,12 @@ __device__ __forceinline__ void mark(const AttentionParams &p, int which, int64_
   if (unit < p.units[which]) marks_of(p, which)[unit] = again;
 }
 
-// Whether any of the pages that hold keys [from, to) is not there; they are looked at by the whole workgroup. The kernels read another page in its place.
+// Whether any of the pages that hold keys [from, to) is not there; they are looked at by the whole workgroup. The kernels read another page in its place. (Blocks of keys
+// begin at multiples of 64, which may be before the first key that a window leaves to see: `from` is that key, what pages before it are does not matter.)
 __device__ __forceinline__ int missing_page(const AttentionParams &p, const int32_t *table, int from, int to)
 {
   bool missing = false;
-  for (int i = (from >> p.page_shift) + threadIdx.x; i <= (to - 1) >> p.page_shift; i += kThreads) missing |= static_cast<uint32_t>(table[i]) >= static_cast<uint32_t>(p.cache.pages);
+  for (int i = (from >> p.page_shift) + threadIdx.x; from < to && i <= (to - 1) >> p.page_shift; i += kThreads) missing |= static_cast<uint32_t>(table[i]) >= static_cast<uint32_t>(p.cache.pages);
   if (missing && p.status) atomicOr(p.status, ITER_BAD_PAGE);
   return missing;
 }

@@ -297,7 +297,7 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
 
     int again = 0;
     if (from < to) {
-      again = missing_page(p, table, from, to);
+      again = missing_page(p, table, max(from, tile_from), to);
       key_loader.begin(head);
       value_loader.begin(head);
       int buffer = 0;                                           // kBuffer for the second one; of the block whose values are due

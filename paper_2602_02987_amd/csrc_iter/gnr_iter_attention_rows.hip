@@ -265,14 +265,14 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_row
     x += last - first;
     // what the tile's tokens see: the last one's end, and what all of them see
     const int first_pos = rq.base + tile * 16 / p.group, last_pos = rq.base + min(rq.tokens - 1, (tile * 16 + 15) / p.group);
-    const int all_end = min(first_pos + 1, rq.end), all_begin = p.window ? last_pos - p.window + 1 : 0;
+    const int all_end = min(first_pos + 1, rq.end), all_begin = p.window ? last_pos - p.window + 1 : 0, any_begin = p.window ? first_pos - p.window + 1 : 0;
     const int from = rq.begin + first * RowsShape::kKeys, stop = min(min(rq.end, last_pos + 1), rq.begin + last * RowsShape::kKeys);
     const int32_t *table = p.batch.page_table + r * p.batch.table_stride;
     const int row = min(tile * 16 + rows.n, all_rows - 1), pos = rq.base + row / p.group;   // (rows beyond the last repeat it; nobody reads them)
     rows.begin(p, head, static_cast<const uint16_t *>(p.q.data) + static_cast<int64_t>(rq.first + row / p.group) * p.q.token_stride + (head * p.group + row % p.group) * p.q.head_stride);
     int again = 0;
     if (from < stop) {
-      again = missing_page(p, table, from, stop);
+      again = missing_page(p, table, max(from, any_begin), stop);
       // the pages of 32 blocks of this wave at a time: lane 2 i + t holds the t-th sixteen's of the i-th
       int pages_ahead = 0, step = 0, pages[2] = {0, 0};
       const auto look_up = [&](int k0) {
@@ -313,7 +313,7 @@ __global__ void __launch_bounds__(kThreads, rows_blocks(kDim)) gnr_attention_row
               for (int i = 0; i < 4; ++i) s[t][i] = 16 * t + i >= see_begin && 16 * t + i < see_end ? s[t][i] : -INFINITY;
             // A weight of zero does not silence a NaN or an infinity: where any stands among values that not every row sees, the
             // rows are computed again by the kernel that joins.
-            again |= rows.clear_values(k0, p.window ? first_pos - p.window + 1 : 0, stop) && first_pos != last_pos;
+            again |= rows.clear_values(k0, any_begin, stop) && first_pos != last_pos;
           }
           uint32_t w[4];
           rows.weigh(s, w, p.scale_log2);

@@ -5,7 +5,7 @@ import torch
 
 import iteration_reference as R
 from paper_2602_02987_amd import iteration as I
-from test_gpu_iteration import DEV, _adapter_case, _adapters_close
+from test_gpu_iteration import DEV, _adapter_case, _adapters_close, _attention_case, _close, _reference
 
 pytestmark = pytest.mark.gpu
 
@@ -46,3 +46,28 @@ def test_adapters_overlap_with_other_strides():
     x.copy_(dev[0])
     I.adapters(x, *dev[1:], out=out)
     _adapters_close(out, data)
+
+
+# ---- attention
+
+# (heads, kv_heads, dim, page, q type, cache, new tokens, cached tokens, window)
+WINDOWS = [(8, 2, 128, 16, "bf16", "bf16", [1, 3, 70], [1000, 333, 700], 51), (4, 1, 64, 1, "fp16", "fp8", [1, 1, 40], [300, 90, 150], 21), (4, 2, 256, 8, "bf16", "fp8", [2, 1, 30], [130, 65, 190], 3),
+           (8, 2, 128, 32, "fp16", "fp16", [1, 17, 200], [97, 127, 500], 1), (2, 2, 64, 16, "bf16", "bf16", [1, 16], [2000, 900], 700)]
+
+
+@pytest.mark.parametrize("case", WINDOWS, ids=lambda c: f"{c[0]}x{c[1]}x{c[2]}-page{c[3]}-{c[4]}-{c[5]}-{sum(c[6])}t-w{c[8]}")
+def test_pages_before_every_window_do_not_matter(case):
+    """A server has given away the pages that no token sees any more: their entries of the table are no pages."""
+    case = (*case, False)
+    q, cache, table, start, length, window = _attention_case(case, 31)
+    k, v, ke, ve = cache
+    gone = table.clone()
+    for r, (n, kv) in enumerate(zip(case[6], case[7])):
+        gone[r, :max(0, kv - n - window + 1) // case[3]] = -1
+        gone[r, -(-kv // case[3]):] = -1
+    assert (gone < 0).any()
+    status = I.new_status(DEV)
+    got = [I.attention(q.to(DEV), k, v, t.to(DEV), start.to(DEV), length.to(DEV), ke, ve, window=window, status=status) for t in (table, gone)]
+    I.check(status)
+    assert torch.equal(*got)
+    _close(got[0], *_reference(q, cache, table, start, length, window))
