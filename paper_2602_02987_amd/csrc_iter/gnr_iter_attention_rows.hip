@@ -194,6 +194,7 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < kValWords; ++i) vw[j][i] = in ? vw[j][i] : 0;
       if constexpr (kFp8) {
+        vs[j] = in ? vs[j] : 127;                               // (zeros times a factor that is no number are none)
         const float scale = exponent_scale(vs[j]);
 #pragma unroll
         for (int i = 0; i < kValWords; ++i) strange |= no_number<T>(T::template from_e4m3<false>(vw[j][i], scale)) || no_number<T>(T::template from_e4m3<true>(vw[j][i], scale));

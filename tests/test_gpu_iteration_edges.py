@@ -71,3 +71,24 @@ def test_pages_before_every_window_do_not_matter(case):
     I.check(status)
     assert torch.equal(*got)
     _close(got[0], *_reference(q, cache, table, start, length, window))
+
+
+@pytest.mark.parametrize("byte", [255, 0])
+@pytest.mark.parametrize("dim", [64, 128, 256])
+def test_exponents_that_nobody_looks_at(dim, byte):
+    """The bytes of places beyond a request's last token and before its window are whatever the memory held."""
+    for window in (0, 19):
+        case = (4, 2, dim, 16, "bf16", "fp8", [1, 1, 3, 40], [50, 300, 29, 75], window, False)
+        q, cache, table, start, length, _ = _attention_case(case, 37)
+        ref = _reference(q, cache, table, start, length, window)
+        k, v, ke, ve = cache
+        seen = torch.zeros((k.shape[0], 16), dtype=torch.bool)
+        for r, (n, kv) in enumerate(zip(case[6], case[7])):
+            for j in range(max(0, kv - n - window + 1) if window else 0, kv):
+                seen[int(table[r, j // 16]), j % 16] = True
+        pages, places = (~seen).nonzero(as_tuple=True)
+        for t, e in ((k, ke), (v, ve)):
+            t.view(torch.uint8)[pages.to(DEV), :, places.to(DEV)] = 0x7F if byte else 0x38
+            e[pages.to(DEV), :, places.to(DEV)] = byte
+        got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, window=window)
+        _close(got, *ref)
