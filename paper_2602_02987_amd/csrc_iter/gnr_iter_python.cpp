@@ -5,6 +5,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
@@ -54,9 +55,12 @@ struct On {
   void *stream() const { return c10::hip::getCurrentHIPStream(device.index()).stream(); }
 };
 
-// Nothing here has a backward pass: better no result than one that gradients do not flow through.
+// Nothing here has derivatives: better no result than one that gradients (or the tangents of forward mode, which torch.no_grad() leaves on) do not flow through.
 void no_gradient(std::initializer_list<const Tensor *> tensors)
 {
+  if (c10::AutogradState::get_tls_state().get_fw_grad_mode())
+    for (const Tensor *t : tensors)
+      TORCH_CHECK_VALUE(!t || !t->_fw_grad(0).defined(), "the iteration operators have no forward-mode derivative: call them with the primals alone");
   if (!c10::GradMode::is_enabled()) return;
   for (const Tensor *t : tensors)
     TORCH_CHECK_VALUE(!t || !t->requires_grad(), "the iteration operators have no backward pass: call them under torch.no_grad() or with detached tensors");

@@ -1,7 +1,7 @@
 """The operators of one batch iteration: what a simulated server stands for, on the GPU (include/gnr_iter.h).
 
 Argument marshalling only, like `binding`: the work runs in the library's HIP kernels, on torch's current stream of the
-tensors' device, and has no backward pass (tensors that require gradients are refused outside `torch.no_grad()`). PyTorch provides the tensors, among them outputs and workspaces that are not given. Nothing waits for the GPU
+tensors' device, and has no derivatives (tensors that require gradients are refused outside `torch.no_grad()`, those with a forward-mode tangent always). PyTorch provides the tensors, among them outputs and workspaces that are not given. Nothing waits for the GPU
 but `check`. The marshalling itself is compiled (csrc_iter/gnr_iter_python.cpp); ValueError is its word for arguments that do not fit
 each other, SimError the library's.
 
