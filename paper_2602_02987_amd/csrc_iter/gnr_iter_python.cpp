@@ -171,7 +171,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
   HANDLE_TH_ERRORS
   want(n, 8);
   const Tensor &kc = *tensor(a[0], "k_cache"), &vc = *tensor(a[1], "v_cache"), &slots = *tensor(a[2], "slots");
-  no_gradient({&kc, &vc});
+  no_gradient({&kc, &vc, optional(a[6], "k"), optional(a[7], "v")});
   const On on(kc);
   const iter_cache c = cache(kc, vc, optional(a[3], "k_exp"), optional(a[4], "v_exp"), on);
   const int64_t wanted = integer(a[5], "dtype");
@@ -195,7 +195,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
   want(n, 14);
   const Tensor &q = *tensor(a[0], "q"), &kc = *tensor(a[1], "k_cache"), &vc = *tensor(a[2], "v_cache"), &table = *tensor(a[3], "page_table");
   const Tensor &start = *tensor(a[4], "q_start"), &length = *tensor(a[5], "kv_len");
-  no_gradient({&q, &kc, &vc});
+  no_gradient({&q, &kc, &vc, optional(a[11], "out")});
   const On on(q);
   const iter_cache c = cache(kc, vc, optional(a[6], "k_exp"), optional(a[7], "v_exp"), on);
   const at::ScalarType type = q.scalar_type();
@@ -236,7 +236,7 @@ PyObject *adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
   const Tensor &x = *tensor(a[0], "x"), &base = *tensor(a[1], "base"), &down = *tensor(a[2], "down"), &up = *tensor(a[3], "up"), &scale = *tensor(a[4], "scale");
   const Tensor &start = *tensor(a[5], "q_start"), &which = *tensor(a[6], "adapter");
   TORCH_CHECK_VALUE(x.dim() == 2 && down.dim() == 3 && up.dim() == 3 && which.dim() == 1, "x has two dimensions, down and up three, adapter one");
-  no_gradient({&x, &base, &down, &up, &scale});
+  no_gradient({&x, &base, &down, &up, &scale, optional(a[7], "out")});
   const On on(x);
   const at::ScalarType type = x.scalar_type();
   const int64_t tokens = x.size(0), wi = x.size(1), count = down.size(0), rank = down.size(1), wo = up.size(1), requests = which.size(0);

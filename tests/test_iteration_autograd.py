@@ -35,3 +35,13 @@ def test_tangents_of_forward_mode_are_refused():
                 call()
             with fw._set_fwd_grad_enabled(False), pytest.raises(ValueError, match="GPU"):   # (the next thing that is wrong)
                 call()
+
+
+def test_results_that_require_gradients_are_refused():
+    rows, y = (torch.zeros(s, dtype=torch.bfloat16, requires_grad=True) for s in ((3, 2, 64), (3, 64)))
+    calls = _calls("cpu")
+    for name, kw in (("kv_read", dict(k=rows)), ("kv_read", dict(v=rows)), ("attention", dict(out=rows)), ("adapters", dict(out=y))):
+        with pytest.raises(ValueError, match="backward"):
+            calls[name](**kw)
+        with torch.no_grad(), pytest.raises(ValueError, match="GPU"):   # (the next thing that is wrong)
+            calls[name](**kw)
