@@ -66,6 +66,14 @@ void no_gradient(std::initializer_list<const Tensor *> tensors)
     TORCH_CHECK_VALUE(!t || !t->requires_grad(), "the iteration operators have no backward pass: call them under torch.no_grad() or with detached tensors");
 }
 
+// What a call is about to write counts as written, as by torch's own operators in place: a backward pass that kept it from before says so instead of using
+// what it holds now. (Inference tensors have nothing that counts.)
+void written(std::initializer_list<const Tensor *> tensors)
+{
+  for (const Tensor *t : tensors)
+    if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+}
+
 // a dimension of one element has no stride that matters
 int64_t step_of(const Tensor &t, int64_t i) { return t.size(i) > 1 ? t.stride(i) : 0; }
 
@@ -159,6 +167,7 @@ PyObject *kv_write(PyObject *, PyObject *const *a, Py_ssize_t n)
   const int64_t tokens = k.dim() ? k.size(0) : 0;
   const iter_rows kr = rows(k, tokens, c.kv_heads, c.head_dim, k.scalar_type(), "k", on), vr = rows(v, tokens, c.kv_heads, c.head_dim, k.scalar_type(), "v", on);
   const auto *at = static_cast<const int64_t *>(numbers(slots, tokens, at::kLong, "slots", on));
+  written({&kc, &vc, optional(a[5], "k_exp"), optional(a[6], "v_exp")});
   const int rc = iter_kv_write(&c, type_of(k.scalar_type()), &kr, &vr, at, tokens, on.stream());
   if (rc != SIM_OK) return error(rc);
   Py_RETURN_NONE;
@@ -182,6 +191,7 @@ PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n)
   const auto make = [&](const Tensor *given) { return given ? *given : at::empty({tokens, c.kv_heads, c.head_dim}, at::TensorOptions().dtype(type).device(on.device)); };
   const Tensor k = make(optional(a[6], "k")), v = make(optional(a[7], "v"));
   const iter_rows kr = rows(k, tokens, c.kv_heads, c.head_dim, type, "k", on), vr = rows(v, tokens, c.kv_heads, c.head_dim, type, "v", on);
+  written({optional(a[6], "k"), optional(a[7], "v")});
   const int rc = iter_kv_read(&c, type_of(type), &kr, &vr, at, tokens, on.stream());
   if (rc != SIM_OK) return error(rc);
   return Py_BuildValue("(NN)", a[6] == Py_None ? THPVariable_Wrap(k) : (Py_INCREF(a[6]), a[6]), a[7] == Py_None ? THPVariable_Wrap(v) : (Py_INCREF(a[7]), a[7]));
@@ -221,6 +231,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
   int rc = iter_attention_bytes(&c, &b, static_cast<int>(heads), &need);
   if (rc != SIM_OK) return error(rc);
   const Workspace work(optional(a[12], "workspace"), need, on);
+  written({given, optional(a[12], "workspace"), optional(a[13], "status")});
   rc = iter_attention(&c, &b, type_of(type), static_cast<int>(heads), &qr, &outr, scale, window, work.data, work.bytes, status_word(optional(a[13], "status"), on), on.stream());
   if (rc != SIM_OK) return error(rc);
   if (given) { Py_INCREF(a[11]); return a[11]; }
@@ -259,6 +270,7 @@ PyObject *adapters(PyObject *, PyObject *const *a, Py_ssize_t n)
   int rc = iter_adapters_bytes(&s, tokens, &need);
   if (rc != SIM_OK) return error(rc);
   const Workspace work(optional(a[8], "workspace"), need, on);
+  written({given, optional(a[8], "workspace"), optional(a[9], "status")});
   rc = iter_adapters(&s, type_of(type), static_cast<int>(requests), tokens, q, w, x.data_ptr(), step_of(x, 0), base.data_ptr(), step_of(base, 0), out.data_ptr(), step_of(out, 0),
                      work.data, work.bytes, status_word(optional(a[9], "status"), on), on.stream());
   if (rc != SIM_OK) return error(rc);

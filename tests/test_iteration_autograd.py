@@ -45,3 +45,35 @@ def test_results_that_require_gradients_are_refused():
             calls[name](**kw)
         with torch.no_grad(), pytest.raises(ValueError, match="GPU"):   # (the next thing that is wrong)
             calls[name](**kw)
+
+
+@pytest.mark.gpu
+def test_what_is_written_counts_as_written():
+    dev = "cuda:0"
+    calls, status = _calls(dev), I.new_status(dev)
+    rows, other = (torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=dev) for _ in range(2))
+    y = torch.zeros((3, 64), dtype=torch.bfloat16, device=dev)
+    work = torch.zeros(1 << 24, dtype=torch.uint8, device=dev)
+    for name, kw in (("kv_read", dict(k=rows, v=other)), ("attention", dict(out=rows, status=status, workspace=work)), ("adapters", dict(out=y, status=status, workspace=work))):
+        before = {n: t._version for n, t in kw.items()}
+        calls[name](**kw)
+        assert {n: t._version > before[n] for n, t in kw.items()} == {n: True for n in kw}, name
+    k, v, ke, ve = I.new_cache(4, 2, 16, 64, torch.float8_e4m3fn, device=dev)
+    slots = torch.zeros(3, dtype=torch.int64, device=dev)
+    slots[1:] = torch.tensor([5, 17], device=dev)
+    before = [t._version for t in (k, v, ke, ve)]
+    I.kv_write(rows, other, k, v, slots, ke, ve)
+    assert all(t._version > b for t, b in zip((k, v, ke, ve), before))
+    I.kv_read(k, v, slots, ke, ve)
+    assert [t._version for t in (k, v, ke, ve)] == [b + 1 for b in before]          # reading is not writing
+    # a product that kept its factor for the backward pass
+    w = torch.ones((3, 2, 64), dtype=torch.bfloat16, device=dev, requires_grad=True)
+    z = (w * rows).sum()
+    I.kv_read(k, v, slots, ke, ve, k=rows)
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        z.backward()
+    with torch.inference_mode():
+        kept = torch.zeros((3, 2, 64), dtype=torch.bfloat16, device=dev)
+        I.kv_read(k, v, slots, ke, ve, k=kept)
+    I.kv_read(k, v, slots, ke, ve, k=kept)                                          # an inference tensor, outside
+    assert torch.equal(kept, rows)
