@@ -5,6 +5,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <ATen/ATen.h>
+#include <ATen/MemoryOverlap.h>
 #include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/hip/HIPFunctions.h>
@@ -67,9 +68,11 @@ void no_gradient(std::initializer_list<const Tensor *> tensors)
 }
 
 // What a call is about to write counts as written, as by torch's own operators in place: a backward pass that kept it from before says so instead of using
-// what it holds now. (Inference tensors have nothing that counts.)
+// what it holds now. (Inference tensors have nothing that counts.) Rows that share memory (an expanded tensor) would be left with any one's values: refused.
 void written(std::initializer_list<const Tensor *> tensors)
 {
+  for (const Tensor *t : tensors)
+    TORCH_CHECK_VALUE(!t || at::has_internal_overlap(*t) != at::MemOverlap::Yes, "a tensor that is written has elements that share memory");
   for (const Tensor *t : tensors)
     if (t && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
 }

@@ -92,3 +92,25 @@ def test_exponents_that_nobody_looks_at(dim, byte):
             e[pages.to(DEV), :, places.to(DEV)] = byte
         got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, window=window)
         _close(got, *ref)
+
+
+# ---- what is refused before anything is launched
+
+def test_results_whose_rows_share_memory_are_refused():
+    k, v, ke, ve = I.new_cache(4, 2, 16, 64, torch.float8_e4m3fn, device=DEV)
+    slots = torch.tensor([0, 5, 17], device=DEV)
+    rows = torch.ones((3, 2, 64), dtype=torch.bfloat16, device=DEV)
+    start, length, table = (torch.tensor(n, dtype=torch.int32, device=DEV) for n in ([0, 3], [3], [[0]]))
+    y = torch.ones((3, 64), dtype=torch.bfloat16, device=DEV)
+    down, up = (torch.ones(s, dtype=torch.bfloat16, device=DEV) for s in ((2, 8, 64), (2, 64, 8)))
+    a = (y, y, down, up, torch.ones(2, device=DEV), start, length - 3)
+    one, head = torch.zeros((1, 2, 64), dtype=torch.bfloat16, device=DEV).expand(3, 2, 64), torch.zeros((3, 1, 64), dtype=torch.bfloat16, device=DEV).expand(3, 2, 64)
+    for call in (lambda: I.attention(rows, k, v, table, start, length, ke, ve, out=one), lambda: I.attention(rows, k, v, table, start, length, ke, ve, out=head),
+                 lambda: I.kv_read(k, v, slots, ke, ve, k=one), lambda: I.kv_read(k, v, slots, ke, ve, v=head), lambda: I.adapters(*a, out=y[:1].expand(3, 64)),
+                 lambda: I.kv_write(rows, rows, k[:, :1].expand(4, 2, 16, 64), v, slots, ke, ve), lambda: I.kv_write(rows, rows, k, v, slots, ke[:1].expand(4, 2, 16), ve)):
+        with pytest.raises(ValueError, match="share memory"):
+            call()
+    # inputs may be expanded
+    I.kv_write(one, head, k, v, slots, ke, ve)
+    assert I.attention(one, k[:, :1].expand(4, 2, 16, 64), v, table, start, length, ke, ve).shape == (3, 2, 64)
+    assert torch.equal(I.adapters(y[:1].expand(3, 64), *a[1:]), I.adapters(*a))
