@@ -92,15 +92,21 @@ class Server:
         self._free += self._pages.pop(r)
         del self._length[r], self._class[r]
 
+    def _missing(self, r: int, n: int) -> int:
+        """Pages that request r lacks for n tokens more."""
+        return -(-(self._length[r] + n) // self.block.page) - len(self._pages[r])
+
     def _grow(self, r: int, n: int) -> range:
         """Room for n tokens more; their positions."""
-        at, page = self._length[r], self.block.page
-        missing = -(-(at + n) // page) - len(self._pages[r])
-        if missing > len(self._free):
-            raise MemoryError(f"the cache has {len(self._free)} pages left, request {r} needs {missing}")
+        at, missing = self._length[r], self._missing(r, n)
+        self._need(missing)
         self._pages[r] += [self._free.pop() for _ in range(missing)]
         self._length[r] = at + n
         return range(at, at + n)
+
+    def _need(self, pages: int) -> None:
+        if pages > len(self._free):
+            raise MemoryError(f"the cache has {len(self._free)} pages left, {pages} are needed")
 
     def _slots(self, r: int, positions: Sequence[int]) -> List[int]:
         page, pages = self.block.page, self._pages[r]
@@ -110,7 +116,9 @@ class Server:
         return torch.tensor(numbers, dtype=dtype).to(self.device)
 
     def plan(self, batch: Sequence[Tuple[int, int]]) -> Plan:
-        """Makes room for an iteration that brings n tokens of request r for every (r, n): 1 for a decode, a chunk's for the prefill."""
+        """Makes room for an iteration that brings n tokens of request r for every (r, n): 1 for a decode, a chunk's for the prefill. A batch that does not
+        fit raises MemoryError and leaves every request as it was: a longer one would have tokens that were never written."""
+        self._need(sum(self._missing(r, n) for r, n in batch))
         slots, start = [], [0]
         for r, n in batch:
             slots += self._slots(r, self._grow(r, n))
@@ -138,12 +146,18 @@ class Server:
 
     @torch.no_grad()
     def move(self, r: int, to: "Server") -> int:
-        """Moves a request with its cache to another server; its number there."""
+        """Moves a request with its cache to another server; its number there. If that one has no room for it, or a cache that is not
+        made for its rows, nothing changes on either."""
         n = self._length[r]
+        to._need(-(-n // to.block.page))
         k, v = iteration.kv_read(self.k, self.v, self._whole(self._slots(r, range(n)), torch.int64), self.k_exp, self.v_exp, dtype=self.block.dtype)
         there = to.admit(self._class[r])
         slots = to._whole(to._slots(there, to._grow(there, n)), torch.int64)
-        iteration.kv_write(k, v, to.k, to.v, slots, to.k_exp, to.v_exp)
+        try:
+            iteration.kv_write(k, v, to.k, to.v, slots, to.k_exp, to.v_exp)
+        except Exception:
+            to.leave(there)
+            raise
         self.leave(r)
         return there
 
