@@ -118,6 +118,10 @@ class Server:
     def plan(self, batch: Sequence[Tuple[int, int]]) -> Plan:
         """Makes room for an iteration that brings n tokens of request r for every (r, n): 1 for a decode, a chunk's for the prefill. A batch that does not
         fit raises MemoryError and leaves every request as it was: a longer one would have tokens that were never written."""
+        if len({r for r, _ in batch}) < len(batch):
+            raise ValueError("a batch has a request once at most: the positions of its tokens are the last ones of its cache")
+        if any(n < 0 for _, n in batch):
+            raise ValueError("a request cannot bring fewer than no tokens")
         self._need(sum(self._missing(r, n) for r, n in batch))
         slots, start = [], [0]
         for r, n in batch:

@@ -54,3 +54,17 @@ def test_a_request_that_another_cache_refuses_stays(monkeypatch):
     with pytest.raises(ValueError):
         one.move(r, two)
     assert (_state(one), _state(two)) == before
+
+
+def test_batches_that_make_no_sense_are_refused():
+    s = _server(4)
+    a, b = s.admit(0), s.admit(0)
+    s.plan([(a, 20), (b, 10)])
+    before = _state(s)
+    for batch in ([(a, 1), (b, 1), (a, 1)], [(a, -3)], [(b, 1), (a, -1)]):
+        with pytest.raises(ValueError):
+            s.plan(batch)
+        assert _state(s) == before
+    with pytest.raises(KeyError):
+        s.plan([(a, 1), (99, 1)])
+    assert _state(s) == before and s.plan([]).tokens == 0 and s.plan([(a, 0)]).kv_len.tolist() == [20]
