@@ -197,3 +197,44 @@ def test_pages_that_are_missing_count_as_absent(case, bad, scale):
     got = _attend(*data, window=case[8], scale=scale, status=status)
     assert int(status.item()) == I.BAD_PAGE
     _close(got, *_reference(*data, case[8], scale, absent))
+
+
+def test_as_many_requests_as_a_batch_can_have():
+    """1024 requests of all kinds: what the kernels keep for each of them still fits beside their tiles, for every head size."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(59)
+    for dim, kind in ((64, "bf16"), (128, "fp8"), (256, "bf16"), (256, "fp8")):
+        q_len = [(1, 1, 2, 0, 1, 20)[i % 6] for i in range(1024)]
+        case = (4, 1, dim, 16, "bf16", kind, q_len, [n + 7 * i % 90 for i, n in enumerate(q_len)], 0)
+        data = _case(case, 61, rising=False)
+        status = I.new_status(DEV)
+        got = _attend(*data, status=status)
+        I.check(status)
+        _close(got, *_reference(*data))
+
+
+@pytest.mark.parametrize("rank", [16, 64, 128])
+@pytest.mark.parametrize("tokens", [1024, 3000])
+def test_as_many_adapters_as_a_set_can_have(rank, tokens):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(rank)
+    n, width, out = 2048, 64, 520
+    which = torch.randint(-1, n, (1024,), generator=gen, device=DEV, dtype=torch.int32)
+    start = (torch.arange(1025, device=DEV) * tokens // 1024).to(torch.int32)
+    x, base, down, up = ((torch.randn(s, generator=gen, device=DEV) * by).bfloat16() for s, by in (((tokens, width), 1.0), ((tokens, out), 1.0), ((n, rank, width), width ** -0.5),
+                                                                                                 ((n, out, rank), rank ** -0.5)))
+    scale = 0.5 + torch.rand(n, generator=gen, device=DEV)
+    status = I.new_status(DEV)
+    got = I.adapters(x, base, down, up, scale, start, which, status=status)
+    I.check(status)
+    a = which[torch.searchsorted(start, torch.arange(tokens, device=DEV, dtype=torch.int32), right=True) - 1].long()
+    ref, inner, outer = base.double().clone(), torch.zeros_like(base, dtype=torch.float64), torch.zeros_like(base, dtype=torch.float64)
+    for t in range(tokens):
+        if a[t] >= 0:
+            d, u, s, row = down[a[t]].double(), up[a[t]].double(), scale[a[t]].double(), x[t].double()
+            h = d @ row
+            ref[t] += s * (u @ h)
+            inner[t], outer[t] = s * (u.abs() @ (d.abs() @ row.abs())), s * (u.abs() @ h.abs())
+    on_cpu = [t.cpu().double().numpy() for t in (ref, base, inner, outer)]
+    bound = R.adapters_bound(*on_cpu, torch.bfloat16, width, rank)
+    _close(got, ref, torch.from_numpy(bound).to(DEV))
