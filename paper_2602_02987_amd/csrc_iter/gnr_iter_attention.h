@@ -154,7 +154,7 @@ __device__ __forceinline__ void share_out_chunks(const AttentionParams &p, const
   for (int r = threadIdx.x; r < n; r += kThreads) all += static_cast<int64_t>(tiles_of<ChunkShape>(p, request_of(p, r, &flags), rows, keys)) * keys;
   block_scan<int64_t>(all, sums, before64, all);
   if (flags && p.status && blockIdx.x == 0) atomicOr(p.status, flags);
-  int size = static_cast<int>(max(int64_t(1), (all * p.cache.kv_heads + blocks - 1) / blocks));
+  int size = blocks_of_a_piece(all * p.cache.kv_heads, blocks);
   for (int round = 0; round < 6; ++round) {      // last pieces that are short make it more than there is room for: take longer ones
     int64_t units = 0;
     for (int r = threadIdx.x; r < n; r += kThreads) {

@@ -39,6 +39,15 @@ struct AdapterParams {
   uint32_t *status;
 };
 
+// Blocks of keys of a piece if `all` are shared out over `workgroups`. No request has as many as the most it returns (positions are below 2^30, a block is 64 of them): a
+// batch with more work than pieces of that length then has none of its tiles cut.
+constexpr int blocks_of_a_piece(int64_t all, int workgroups)
+{
+  constexpr int64_t most = int64_t(1) << 25;
+  const int64_t share = (all + workgroups - 1) / workgroups;
+  return static_cast<int>(share < 1 ? 1 : share > most ? most : share);
+}
+
 // All return a sim_err; arguments have been checked.
 int launch_kv_write(const iter_cache &c, int type, const iter_rows &k, const iter_rows &v, const int64_t *slots, int64_t tokens, void *stream);
 int launch_kv_read(const iter_cache &c, int type, const iter_rows &k, const iter_rows &v, const int64_t *slots, int64_t tokens, void *stream);
