@@ -97,8 +97,9 @@ int iter_attention_bytes(const iter_cache *cache, const iter_batch *batch, int h
  * FP16; the cache's type or, for an FP8 cache, either), heads a multiple of kv_heads, and query head h reads kv head
  * h / (heads / kv_heads). The token at position p = kv_len - q_len + i of its request sees positions max(0, p - window + 1) .. p
  * (window = 0: 0 .. p): out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q.k_j). A token that sees nothing gets zeros. What lies
- * where a token does not look (NaN included) does not matter. Scores, sums and outputs are held in 32 bits; the weights are rounded to `type` for
- * the matrix product with the values, relative to the largest of their row. Rows of tokens outside every request (of a batch with
+ * where a token does not look (NaN included) does not matter. Scores, sums and outputs are held in 32 bits. For
+ * the matrix product with the values the weights are the sum of two numbers of `type` each where a request has up to 16 rows (its tokens times query heads of a kv head), and
+ * rounded to one number, relative to the largest of their row, where it has more. Rows of tokens outside every request (of a batch with
  * bounds out of range) are not written. out must not overlap q, nor be the same rows. There is no backward pass. */
 int iter_attention(const iter_cache *cache, const iter_batch *batch, int type, int heads, const iter_rows *q,
                    const iter_rows *out, double scale, int64_t window, void *workspace, size_t bytes, uint32_t *status,

@@ -267,6 +267,8 @@ __global__ void __launch_bounds__(kThreads, chunk_blocks(kDim)) gnr_attention_ch
       }
       return keep;
     };
+    // Weights are rounded to 16 bits for their product, relative to the row's largest (their sum is of 32-bit ones). Held as two numbers each, as in the kernel for few
+    // rows, they would double these products: whole prompt 558 -> 737 us for an error against 64 bits of 1.6e-3 instead of 2.2e-3, where the result's own rounding is 1.6e-3.
     const auto weigh = [&](auto i) GNR_INLINE {                 // scores 2 i and 2 i + 1
       constexpr int j = 2 * (i % 8), word = i % 4;
       const f32x16 &x = i < 8 ? low : high;

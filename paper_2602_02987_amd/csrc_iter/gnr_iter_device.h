@@ -29,7 +29,10 @@ __device__ __forceinline__ To bits(From f)
   return __builtin_bit_cast(To, f);
 }
 
-// The 16-bit types: T::from_e4m3 reads two codes (the lower or upper half of a word) times a power of two, exactly but for
+// The 16-bit types: T::split2 makes two numbers of each of two weights from 0 to 2^15, an upper one (cut off) and what it leaves (rounded), together within 2^-14 of it
+// (bfloat16) or 2^-20 (float16). Neither is zero or negative where the weight counts, so that an infinite value times both is the same infinity: a little less than the weight is cut
+// off, and a lower number that would vanish is float16's smallest. There weights are multiplied by 2^kSplitShift, as their sum is, to have room for lower numbers.
+// T::from_e4m3 reads two codes (the lower or upper half of a word) times a power of two, exactly but for
 // what leaves the type's range; T::to_e4m3 is its inverse, rounded to nearest even, for values within 448 * 2^e.
 struct Bf16 {
   typedef __bf16 elem;
@@ -38,6 +41,13 @@ struct Bf16 {
   static constexpr uint32_t kInf = 0x7F80u;
   static __device__ __forceinline__ float widen(uint32_t w) { return bits<float>(w << 16); }
   static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<__bf16>(a), static_cast<__bf16>(b)}; return bits<uint32_t>(p); }
+  static constexpr float kSplitShift = 0.0f;
+  static __device__ __forceinline__ void split2(float a, float b, uint32_t &upper, uint32_t &lower)
+  {
+    const uint32_t x = bits<uint32_t>(a * 0x1.FFp-1f), y = bits<uint32_t>(b * 0x1.FFp-1f);
+    upper = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    lower = narrow2(a - bits<float>(x & 0xFFFF0000u), b - bits<float>(y & 0xFFFF0000u));
+  }
   static __device__ __forceinline__ f32x4 mfma16(oct a, oct b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(oct a, oct b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
   template <bool kUpper>
@@ -52,6 +62,12 @@ struct Fp16 {
   static constexpr uint32_t kInf = 0x7C00u;
   static __device__ __forceinline__ float widen(uint32_t w) { return static_cast<float>(bits<_Float16>(static_cast<uint16_t>(w))); }
   static __device__ __forceinline__ uint32_t narrow2(float a, float b) { pair p = {static_cast<_Float16>(a), static_cast<_Float16>(b)}; return bits<uint32_t>(p); }
+  static constexpr float kSplitShift = 7.0f;
+  static __device__ __forceinline__ void split2(float a, float b, uint32_t &upper, uint32_t &lower)
+  {
+    upper = bits<uint32_t>(__builtin_amdgcn_cvt_pkrtz(a * 0x1.FFEp-1f, b * 0x1.FFEp-1f));
+    lower = narrow2(fmaxf(a - widen(upper & 0xFFFFu), fminf(a, 0x1p-24f)), fmaxf(b - widen(upper >> 16), fminf(b, 0x1p-24f)));
+  }
   static __device__ __forceinline__ f32x4 mfma16(oct a, oct b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
   static __device__ __forceinline__ f32x16 mfma32(oct a, oct b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
   template <bool kUpper>
