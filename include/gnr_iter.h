@@ -95,7 +95,9 @@ int iter_attention_bytes(const iter_cache *cache, const iter_batch *batch, int h
 
 /* Attention of the batch's tokens over their requests' caches: q and out are [tokens][heads][head_dim] of `type` (BF16 or
  * FP16; the cache's type or, for an FP8 cache, either), heads a multiple of kv_heads, and query head h reads kv head
- * h / (heads / kv_heads). The token at position p = kv_len - q_len + i of its request sees positions max(0, p - window + 1) .. p
+ * h / (heads / kv_heads). Keys and values of an FP8 cache are what iter_kv_read gives in `type`: for FP16
+ * infinite from 65520 on and rounded to multiples of 2^-24, which takes nothing from rows that were written from FP16 and stayed below 63488 (rows of larger or smaller BF16
+ * values belong to BF16 queries). The token at position p = kv_len - q_len + i of its request sees positions max(0, p - window + 1) .. p
  * (window = 0: 0 .. p): out = sum_j w_j v_j / sum_j w_j, w_j = exp(scale * q.k_j). A token that sees nothing gets zeros. What lies
  * where a token does not look (NaN included) does not matter. Scores, sums and outputs are held in 32 bits. For
  * the matrix product with the values the weights are the sum of two numbers of `type` each where a request has up to 16 rows (its tokens times query heads of a kv head), and

@@ -33,7 +33,8 @@ __device__ __forceinline__ To bits(From f)
 // (bfloat16) or 2^-20 (float16). Neither is zero or negative where the weight counts, so that an infinite value times both is the same infinity: a little less than the weight is cut
 // off, and a lower number that would vanish is float16's smallest. There weights are multiplied by 2^kSplitShift, as their sum is, to have room for lower numbers.
 // T::from_e4m3 reads two codes (the lower or upper half of a word) times a power of two, exactly but for
-// what leaves the type's range; T::to_e4m3 is its inverse, rounded to nearest even, for values within 448 * 2^e.
+// what leaves the type's range, in one instruction (the attention kernels take cached rows that way too: powers of two that went through scores and weights instead would cost one
+// for each of these, and change nothing where the rows fit the queries' type); T::to_e4m3 is its inverse, rounded to nearest even, for values within 448 * 2^e.
 struct Bf16 {
   typedef __bf16 elem;
   typedef bf16x2 pair;

@@ -124,7 +124,8 @@ def attention(q, k_cache, v_cache, page_table, q_start, kv_len, k_exp=None, v_ex
               workspace=None, status=None):
     """Attention of a batch's tokens q ([tokens, heads, head_dim]) over their requests' caches: the token at position p of its request sees
     the positions max(0, p - window + 1) .. p (window 0: all up to p). `scale` is 1 / sqrt(head_dim) unless given, `max_q` the longest chunk
-    the host expects (it selects kernels only). Returns [tokens, heads, head_dim], in `out` if given (which must not overlap q)."""
+    the host expects (it selects kernels only). Over an 8-bit cache keys and values are what `kv_read` gives in the type of q. Returns
+    [tokens, heads, head_dim], in `out` if given (which must not overlap q)."""
     if max_q is not None and max_q < 0:
         raise ValueError("max_q has to be 0 or more")
     o = _iteration.attention(q, k_cache, v_cache, page_table, q_start, kv_len, k_exp, v_exp, -1 if max_q is None else max_q, scale, window, out,

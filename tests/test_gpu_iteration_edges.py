@@ -114,3 +114,31 @@ def test_results_whose_rows_share_memory_are_refused():
     I.kv_write(one, head, k, v, slots, ke, ve)
     assert I.attention(one, k[:, :1].expand(4, 2, 16, 64), v, table, start, length, ke, ve).shape == (3, 2, 64)
     assert torch.equal(I.adapters(y[:1].expand(3, 64), *a[1:]), I.adapters(*a))
+
+
+@pytest.mark.parametrize("dim", [64, 128, 256])
+@pytest.mark.parametrize("q_len,kv_len", [([1, 1], [200, 47]), ([2, 60], [90, 150])])
+def test_cached_rows_are_taken_as_they_are_read_back(dim, q_len, kv_len):
+    """float16 queries over 8-bit rows whose exponents reach far below (rounded to multiples of 2^-24) and above what float16 holds exactly."""
+    case = (4, 2, dim, 16, "fp16", "fp8", q_len, kv_len, 0, False)
+    q, cache, table, start, length, _ = _attention_case(case, 73)
+    k, v, ke, ve = cache
+    gen = torch.Generator()
+    gen.manual_seed(dim)
+    for e, low in ((ke, 103), (ve, 106)):                       # keys around 2^-18, values around 2^-15, down to float16's last bits
+        e.copy_(torch.randint(low, low + 5, e.shape, generator=gen).to(torch.uint8))
+    scale = 2.0 ** 13 / dim ** 0.5                              # scores as usual
+    slots = torch.arange(k.shape[0] * 16, device=DEV)
+    read = [t.cpu().double().numpy().reshape(k.shape[0], 16, 2, dim).transpose(0, 2, 1, 3) for t in I.kv_read(k, v, slots, ke, ve, dtype=torch.float16)]
+    exact = [R.cache_values(t, e) for t, e in ((k, ke), (v, ve))]
+    assert (read[1] != exact[1]).any() and np.abs(read[1] - exact[1]).max() <= 2.0 ** -25
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, scale=scale)
+    ref, parts = R.attention(q.double().numpy(), *read, table.numpy(), start.numpy(), length.numpy(), scale)
+    _close(got, ref, R.attention_bound(ref, parts, torch.float16, dim))
+    # values of 40000 and more, whose average float16 holds
+    ve.fill_(127 + 7)
+    read = [t.cpu().double().numpy().reshape(k.shape[0], 16, 2, dim).transpose(0, 2, 1, 3) for t in I.kv_read(k, v, slots, ke, ve, dtype=torch.float16)]
+    assert np.abs(read[1]).max() > 4e4
+    got = I.attention(q.to(DEV), k, v, table.to(DEV), start.to(DEV), length.to(DEV), ke, ve, scale=scale)
+    ref, parts = R.attention(q.double().numpy(), *read, table.numpy(), start.numpy(), length.numpy(), scale)
+    _close(got, ref, R.attention_bound(ref, parts, torch.float16, dim))
