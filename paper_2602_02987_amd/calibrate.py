@@ -5,8 +5,8 @@ c0 + c_pre * prefill_tokens + c_dec * n_decode to them; what it prints can be ha
 
 `Server` is the block itself: a paged cache (8-bit or as the activations), projections that all requests share (plain matrix products of the
 library), an adapter for each class beside them, and attention of all tokens of an iteration over their requests' caches. A request can be
-moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time. A model's feed-forward blocks are not
-in these times.
+moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time. The law is that of a model's attention blocks: its
+feed-forward blocks are not in these times.
 """
 from __future__ import annotations
 
@@ -54,6 +54,16 @@ class Weights:
         self.qkv_adapter = of(b.classes, b.rank, b.width), of(b.classes, into, b.rank)
         self.out_adapter = of(b.classes, b.rank, b.width), of(b.classes, b.width, b.rank)
         self.scale = torch.ones(b.classes, device=device)
+
+    def copy(self) -> "Weights":
+        """The same numbers in other memory."""
+        w = Weights.__new__(Weights)
+        for name, value in vars(self).items():
+            setattr(w, name, tuple(t.clone() for t in value) if isinstance(value, tuple) else value.clone())
+        return w
+
+    def bytes(self) -> int:
+        return sum(t.nbytes for value in vars(self).values() for t in (value if isinstance(value, tuple) else (value,)))
 
 
 @dataclass
@@ -177,10 +187,18 @@ def fit(samples: Sequence[Tuple[int, int, float]]) -> dict:
     return dict(c0=float(c[0]), c_pre=float(c[1]), c_dec=float(c[2]), residual=float((np.abs(a @ c - s[:, 2]) / s[:, 2]).max()))
 
 
-def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context: int, passes: int = 20, device="cuda") -> List[Tuple[int, int, float]]:
-    """Seconds of an iteration for every (chunk, decodes) but (0, 0), every request with `context` tokens before it."""
+_LAST_LEVEL_CACHE = 256 << 20
+
+
+def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context: int, passes: int = 20, device="cuda", layers: int = 32) -> List[Tuple[int, int, float]]:
+    """Seconds of an iteration of one block on the GPU for every (chunk, decodes) but (0, 0), every request with `context` tokens before it.
+
+    A model goes through the weights and caches of all its layers before it comes back to one's, so the passes go through as many blocks as a model of `layers` layers
+    has, or as few as are twice the chip's last-level cache."""
     most = max(decodes) + 1
-    server = Server(block, Weights(block, device=device), most * -(-(context + max(chunks) + 1) // block.page), device)
+    pages = most * -(-(context + max(chunks) + 1) // block.page)
+    first = Weights(block, device=device)
+    servers = [Server(block, w, pages, device) for w in [first] + [first.copy() for _ in range(min(layers, -(-2 * _LAST_LEVEL_CACHE // first.bytes())) - 1)]]
     gen = torch.Generator(device=device)
     gen.manual_seed(1)
     samples = []
@@ -188,23 +206,30 @@ def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context
         for n in decodes:
             if chunk + n == 0:
                 continue
-            requests = [server.admit(i % block.classes) for i in range(n + (chunk > 0))]
-            for r in requests:                                  # what came before
-                p = server.plan([(r, context)])
-                server.iterate(torch.randn((context, block.width), generator=gen, device=device).to(block.dtype), p)
-            p = server.plan([(r, 1) for r in requests[:n]] + [(r, chunk) for r in requests[n:]])
-            x = torch.randn((p.tokens, block.width), generator=gen, device=device).to(block.dtype)
+            before = torch.randn((context, block.width), generator=gen, device=device).to(block.dtype)
+            plans = []
+            for s in servers:
+                requests = [s.admit(i % block.classes) for i in range(n + (chunk > 0))]
+                for r in requests:                              # what came before
+                    s.iterate(before, s.plan([(r, context)]))
+                plans.append(s.plan([(r, 1) for r in requests[:n]] + [(r, chunk) for r in requests[n:]]))
+            x = torch.randn((plans[0].tokens, block.width), generator=gen, device=device).to(block.dtype)
+
+            def run(count):                                     # (the same tokens again: an iteration's time does not depend on that)
+                for i in range(count):
+                    servers[i % len(servers)].iterate(x, plans[i % len(servers)])
+            run(3)
             begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-            for i in range(3 + passes):                         # (the same tokens again: an iteration's time does not depend on that)
-                if i == 3:
-                    begin.record()
-                server.iterate(x, p)
+            begin.record()
+            run(passes)
             end.record()
             end.synchronize()
             samples.append((chunk, n, begin.elapsed_time(end) / passes / 1e3))
-            for r in requests:
-                server.leave(r)
-    iteration.check(server.status)
+            for s in servers:
+                for r in list(s._length):
+                    s.leave(r)
+    for s in servers:
+        iteration.check(s.status)
     return samples
 
 
@@ -217,8 +242,8 @@ def main() -> None:
     a.add_argument("--cache", choices=["fp8", "bf16"], default="fp8")
     o = a.parse_args()
     block = Block(cache=torch.float8_e4m3fn if o.cache == "fp8" else torch.bfloat16)
-    samples = [(c, n, t * o.layers) for c, n, t in measure(block, o.chunks, o.decodes, o.context)]
-    print(json.dumps(dict(fit(samples), layers=o.layers, context=o.context, cache=o.cache, samples=[dict(chunk=c, decodes=n, seconds=t) for c, n, t in samples])))
+    samples = [(c, n, t * o.layers) for c, n, t in measure(block, o.chunks, o.decodes, o.context, layers=o.layers)]
+    print(json.dumps(dict(fit(samples), of="attention blocks", layers=o.layers, context=o.context, cache=o.cache, samples=[dict(chunk=c, decodes=n, seconds=t) for c, n, t in samples])))
 
 
 if __name__ == "__main__":

@@ -1,0 +1,29 @@
+"""What the calibration times: iterations that go through a model's layers."""
+import pytest
+import torch
+
+from paper_2602_02987_amd import calibrate as K
+from paper_2602_02987_amd import iteration as I
+
+SMALL = K.Block(heads=4, kv_heads=2, head_dim=64, rank=8, classes=2, page=16)
+
+
+def test_copies_of_weights_are_the_same_numbers_in_other_memory():
+    w = K.Weights(SMALL, 3, "cpu")
+    c = w.copy()
+    pairs = [(a, b) for name in vars(w) for a, b in (zip(*(getattr(t, name) for t in (w, c))) if isinstance(getattr(w, name), tuple) else [(getattr(w, name), getattr(c, name))])]
+    assert len(pairs) == 7 and all(torch.equal(a, b) and a.data_ptr() != b.data_ptr() for a, b in pairs)
+    assert w.bytes() == sum(a.nbytes for a, _ in pairs) == c.bytes()
+
+
+@pytest.mark.gpu
+def test_passes_go_through_the_layers(monkeypatch):
+    used = []
+    write = I.kv_write
+    monkeypatch.setattr(I, "kv_write", lambda k, v, kc, *a, **kw: used.append(kc.data_ptr()) or write(k, v, kc, *a, **kw))
+    K.measure(SMALL, [16], [2], 20, passes=12, layers=5)
+    last = used[-12:]
+    assert len(set(last)) == 5 and last[:5] == last[5:10] and last[:2] == last[10:]
+    big = K.Block()
+    assert K._LAST_LEVEL_CACHE < 7 * K.Weights(big, device="cuda:0").bytes()
+
