@@ -5,8 +5,8 @@ c0 + c_pre * prefill_tokens + c_dec * n_decode to them; what it prints can be ha
 
 `Server` is the block itself: a paged cache (8-bit or as the activations), projections that all requests share (plain matrix products of the
 library), an adapter for each class beside them, and attention of all tokens of an iteration over their requests' caches. A request can be
-moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time. The law is that of a model's attention blocks: its
-feed-forward blocks are not in these times.
+moved from the server of its prefill to the one of its decode. Weights are random: only sizes matter to the time. The law is that of a model's attention blocks on the
+GPU: its feed-forward blocks and what the host does between launches are not in these times.
 """
 from __future__ import annotations
 
@@ -194,13 +194,15 @@ def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context
     """Seconds of an iteration of one block on the GPU for every (chunk, decodes) but (0, 0), every request with `context` tokens before it.
 
     A model goes through the weights and caches of all its layers before it comes back to one's, so the passes go through as many blocks as a model of `layers` layers
-    has, or as few as are twice the chip's last-level cache."""
+    has, or as few as are twice the chip's last-level cache. What the host takes to launch an iteration, which is longer than one of a few tokens runs, is not in the
+    times: all passes are queued before the first begins."""
     most = max(decodes) + 1
     pages = most * -(-(context + max(chunks) + 1) // block.page)
     first = Weights(block, device=device)
     servers = [Server(block, w, pages, device) for w in [first] + [first.copy() for _ in range(min(layers, -(-2 * _LAST_LEVEL_CACHE // first.bytes())) - 1)]]
     gen = torch.Generator(device=device)
     gen.manual_seed(1)
+    room = torch.zeros(1 << 28, device=device)                  # 1 GiB, to keep the GPU busy while passes are queued
     samples = []
     for chunk in chunks:
         for n in decodes:
@@ -219,18 +221,29 @@ def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context
                 for i in range(count):
                     servers[i % len(servers)].iterate(x, plans[i % len(servers)])
             run(3)
-            begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
-            begin.record()
-            run(passes)
-            end.record()
-            end.synchronize()
-            samples.append((chunk, n, begin.elapsed_time(end) / passes / 1e3))
+            samples.append((chunk, n, _seconds_ahead(lambda: run(passes), room) / passes))
             for s in servers:
                 for r in list(s._length):
                     s.leave(r)
     for s in servers:
         iteration.check(s.status)
     return samples
+
+
+def _seconds_ahead(run, room: torch.Tensor) -> float:
+    """Seconds that the GPU takes for what run() launches, all of which the host has launched by the time the GPU begins with it."""
+    for fills in (8, 32, 128, 512):
+        begin, end = (torch.cuda.Event(enable_timing=True) for _ in range(2))
+        for _ in range(fills):
+            room.add_(1.0)
+        begin.record()
+        run()
+        end.record()
+        late = begin.query()
+        end.synchronize()
+        if not late:
+            return begin.elapsed_time(end) / 1e3
+    raise RuntimeError("the host does not get ahead of the GPU: measure fewer passes at a time")
 
 
 def main() -> None:

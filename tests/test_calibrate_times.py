@@ -1,4 +1,6 @@
-"""What the calibration times: iterations that go through a model's layers."""
+"""What the calibration times: the GPU's part of iterations that go through a model's layers."""
+import time
+
 import pytest
 import torch
 
@@ -27,3 +29,14 @@ def test_passes_go_through_the_layers(monkeypatch):
     big = K.Block()
     assert K._LAST_LEVEL_CACHE < 7 * K.Weights(big, device="cuda:0").bytes()
 
+
+@pytest.mark.gpu
+def test_a_slow_host_is_not_in_the_times(monkeypatch):
+    write = I.kv_write
+
+    def slow(*a, **kw):
+        time.sleep(0.004)
+        return write(*a, **kw)
+    monkeypatch.setattr(I, "kv_write", slow)
+    samples = K.measure(SMALL, [0], [1, 3], 20, passes=3, layers=2)
+    assert all(0 < t < 0.001 for _, _, t in samples), samples
