@@ -1,8 +1,12 @@
 """Builds the simulator's shared library in-tree with hipcc for gfx950."""
 from __future__ import annotations
 
+import importlib.util
 import os
+import shutil
 import subprocess
+import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -76,16 +80,33 @@ def build(verbose: bool = False, force: bool = True, jobs: int | None = None) ->
     if verbose:
         print(" ".join(cmd), flush=True)
     subprocess.check_call(cmd)
-    build_binding(verbose, force)
+    lacking = binding_lacks()
+    if lacking:      # the library and the simulator need none of it
+        print(f"{os.path.basename(BINDING)}, the iteration operators' binding, is not built: there is no {lacking}", file=sys.stderr, flush=True)
+    else:
+        build_binding(verbose, force)
     return LIB
+
+
+def _torch() -> str | None:
+    spec = importlib.util.find_spec("torch")
+    return os.path.dirname(spec.origin) if spec and spec.origin else None
+
+
+def binding_lacks() -> str:
+    """What the binding needs to be compiled and is not installed ("" if nothing): torch with its headers, Python's headers, a host compiler."""
+    torch, cxx = _torch(), os.environ.get("CXX", "g++")
+    if torch is None or not os.path.exists(os.path.join(torch, "include", "ATen", "ATen.h")):
+        return "torch with headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python.h"
+    return "" if shutil.which(cxx) else f"host compiler {cxx}"
 
 
 def build_binding(verbose: bool = False, force: bool = True) -> str:
     """Compiles the iteration operators' binding against the library and the torch that is installed (host code only)."""
-    import importlib.util
-    import sysconfig
     src = os.path.join(CSRC_ITER, "gnr_iter_python.cpp")
-    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    torch = _torch()
     deps = [src, os.path.join(INCLUDE, "gnr_iter.h"), os.path.join(torch, "version.py")]
     if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) > os.path.getmtime(d) for d in deps):
         return BINDING
@@ -108,5 +129,4 @@ def lib_path() -> str:
 
 
 if __name__ == "__main__":
-    import sys
     print(build(verbose=True, force="--changed" not in sys.argv))
