@@ -109,7 +109,7 @@ int iter_attention(const iter_cache *cache, const iter_batch *batch, int type, i
 
 /* Low-rank adapters, beside a projection that all requests share: for the tokens t of request r with a = adapter[r],
  * out[t] = base[t] + scale[a] * up[a] (down[a] x[t]), out[t] = base[t] for a = -1. x is [tokens][width_in], base and out
- * [tokens][width_out] (rows 16-byte aligned; out may be base itself, and either may be or overlap x), down [adapters][rank][width_in] and up
+ * [tokens][width_out] (rows 16-byte aligned; out may be base itself or apart from it, and either may be or overlap x), down [adapters][rank][width_in] and up
  * [adapters][width_out][rank] without gaps, all of `type`; scale fp32. Widths and rank: multiples of 8, rank up to ITER_MAX_RANK. */
 typedef struct {
   int adapters, rank;
@@ -118,6 +118,7 @@ typedef struct {
   const float *scale;                                      /* device */
 } iter_adapter_set;
 
+/* Device bytes of the workspace iter_adapters needs for any such call (whether it uses them goes by the batch and by whether out overlaps x). */
 int iter_adapters_bytes(const iter_adapter_set *set, int64_t tokens, size_t *out_bytes);
 int iter_adapters(const iter_adapter_set *set, int type, int requests, int64_t tokens, const int32_t *q_start,
                   const int32_t *adapter, const void *x, int64_t x_stride, const void *base, int64_t base_stride,

@@ -84,7 +84,7 @@ __device__ __forceinline__ int find_tile(const AdapterParams &p, int tile, bool 
 // of down as the left operand, so that no operand passes through shared memory; the waves' sums are added there. Bound by reading x once, and
 // for few tokens by the latency of a load or two, which is why the elements are shared out over workgroups until the chip is full. Of many tokens
 // a tile takes 64, so that a row of down is read once for them. 8191 tokens, width 4096,
-// rank 32: 25 us (2.8 TB/s); 128 tokens: 6 us. Asking for the next elements before these are multiplied changes nothing.
+// rank 32: 22 us (3.1 TB/s); 128 tokens: 6 us. Asking for the next elements before these are multiplied changes nothing.
 template <class T, int kRankTiles, int kSub>
 __global__ void __launch_bounds__(kThreads) gnr_adapters_down_kernel(const AdapterParams p)
 {
@@ -247,7 +247,7 @@ struct Columns {
 };
 
 // out = base + scale up h of a tile, 128 columns to a wave. Bound by reading base and writing out; base and the rows of up are asked for
-// before h is added up. 8191 tokens, width 6144, rank 32: 52 us (3.9 TB/s).
+// before h is added up. 8191 tokens, width 6144, rank 32: 48 us (4.2 TB/s).
 template <class T, int kRankSteps, int kSub>
 __global__ void __launch_bounds__(kThreads, kRankSteps == 4 ? 2 : 3) gnr_adapters_up_kernel(const AdapterParams p, int splits)
 {

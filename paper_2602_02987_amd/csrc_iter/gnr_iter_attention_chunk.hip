@@ -8,8 +8,8 @@ namespace gnr {
 // rows: S^T = K Q^T leaves a lane with the scores of one row for keys 8 (i / 4) + 4 h + i % 4 (h: half of the wave), and O^T = V^T P^T numbers its
 // keys the same way, so the weights go from one product to the next within registers, and maximum, sum and rescaling of a row stay in its two lanes.
 // V^T is read with the transposing LDS load. Bound by the matrix cores and the vector instructions beside them (exponentials, sums, in 8 bits the widening):
-// 49 and 47 % of the cycles of a whole prompt, 36 and 41 in 8 bits; then by the LDS reads (a byte of keys or values for every 32 rows). A prompt of 8191 tokens, 32 heads over 8: 548 us, 1.0 PFLOP/s of
-// what the mask leaves; 251 tokens after 32517, 28 heads over 4, 8 bits: 158 us with the join, 0.74.
+// 49 and 47 % of the cycles of a whole prompt, 36 and 41 in 8 bits; then by the LDS reads (a byte of keys or values for every 32 rows). A prompt of 8191 tokens, 32 heads over 8: 548 to 570 us (machines differ), 1.0 PFLOP/s of
+// what the mask leaves; 251 tokens after 32517, 28 heads over 4, 8 bits: 161 us with the join, 0.73.
 //   Rows of the LDS blocks are 16-byte pieces in an order that depends on the key, so that the 32 keys of a K operand and the four
 // keys of a transposing load lie in different banks.
 template <int kDim>

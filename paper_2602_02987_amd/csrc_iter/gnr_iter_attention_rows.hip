@@ -9,8 +9,8 @@ namespace gnr {
 // head_dim / 16 neighbouring elements of eight keys' values and swaps halves of registers to have eight keys of one element; no
 // shared memory is used, every byte of the cache goes from memory to the registers of the wave that multiplies it. Each wave takes every
 // fourth block of 32 keys with a running maximum and sum of its own; the waves are joined at the end.
-//   Bound by the memory: sixteen rows of products for a key are far below the matrix rate. 127 decodes of 435000 keys beside a chunk (1.8 GB, 16 bits): 373 us in all,
-// 4.8 TB/s; 32 decodes of 100000 keys in 8 bits: 48 us, 4.3 TB/s. A single decode of 1093 keys takes 9 us: the chain from bounds to page table to keys to values.
+//   Bound by the memory: sixteen rows of products for a key are far below the matrix rate. 127 decodes of 435000 keys beside a chunk (1.8 GB, 16 bits): 374 us in all,
+// 4.8 TB/s; 32 decodes of 100000 keys in 8 bits: 46 us, 4.5 TB/s. A single decode of 1093 keys takes 9 us: the chain from bounds to page table to keys to values.
 template <class T, int kDim, bool kFp8, bool kSmallPages>
 struct Tile {
   static constexpr int kVec = kDim / 16;                        // elements of a value row a lane reads

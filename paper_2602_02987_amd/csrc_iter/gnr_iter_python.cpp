@@ -1,5 +1,5 @@
 // The binding of the iteration operators: argument checks and marshalling of torch tensors in compiled code, because calls for a decode batch are
-// shorter than marshalling in Python takes (kv_write 18 -> 6 us, the kernel 3). Functions take positional arguments, None for what is
+// shorter than marshalling in Python takes (kv_write 17.6 us a call; 3.5 to 4.9 here, of which the kernel is 2.6). Functions take positional arguments, None for what is
 // not given; they return their result, or the library's error as a whole number.
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>

@@ -138,7 +138,7 @@ def attention(q, k_cache, v_cache, page_table, q_start, kv_len, k_exp=None, v_ex
 def adapters(x, base, down, up, scale, q_start, adapter, out=None, workspace=None, status=None):
     """base + scale[a] * up[a] (down[a] x) for the tokens of every request, a = adapter[request] (-1: base as it is). x [tokens, width_in],
     base [tokens, width_out], down [adapters, rank, width_in], up [adapters, width_out, rank], all bfloat16 or all float16; scale float32
-    [adapters], q_start and adapter int32. `out` may be `base`, and may overlap `x`."""
+    [adapters], q_start and adapter int32. `out` may be `base` (or is apart from it), and may overlap `x`."""
     o = _iteration.adapters(x, base, down, up, scale, q_start, adapter, out, workspace, status)
     if type(o) is int:
         raise SimError(o, "iter_adapters")
