@@ -89,6 +89,17 @@ class Server:
         self._pages, self._length, self._class = {}, {}, {}
         self._next = 0
 
+    def bytes(self) -> int:
+        """Of the cache."""
+        return sum(t.nbytes for t in (self.k, self.v, self.k_exp, self.v_exp) if t is not None)
+
+    def copy_cache(self, other: "Server") -> None:
+        """Contents of another server's cache of the same size."""
+        for name in ("k", "v", "k_exp", "v_exp"):
+            mine, its = getattr(self, name), getattr(other, name)
+            if mine is not None and mine is not its:
+                mine.copy_(its)
+
     def admit(self, which: int) -> int:
         """A request of class `which` (-1: without an adapter) that has no tokens yet."""
         r, self._next = self._next, self._next + 1
@@ -199,7 +210,10 @@ def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context
     most = max(decodes) + 1
     pages = most * -(-(context + max(chunks) + 1) // block.page)
     first = Weights(block, device=device)
-    servers = [Server(block, w, pages, device) for w in [first] + [first.copy() for _ in range(min(layers, -(-2 * _LAST_LEVEL_CACHE // first.bytes())) - 1)]]
+    servers = [Server(block, first, pages, device)]
+    each = first.bytes() + servers[0].bytes()
+    fit_in = 1 + int(0.75 * torch.cuda.mem_get_info(device)[0]) // each     # (with the longest caches fewer have to do)
+    servers += [Server(block, first.copy(), pages, device) for _ in range(min(layers, fit_in, -(-2 * _LAST_LEVEL_CACHE // first.bytes())) - 1)]
     gen = torch.Generator(device=device)
     gen.manual_seed(1)
     room = torch.zeros(1 << 28, device=device)                  # 1 GiB, to keep the GPU busy while passes are queued
@@ -212,8 +226,11 @@ def measure(block: Block, chunks: Sequence[int], decodes: Sequence[int], context
             plans = []
             for s in servers:
                 requests = [s.admit(i % block.classes) for i in range(n + (chunk > 0))]
-                for r in requests:                              # what came before
-                    s.iterate(before, s.plan([(r, context)]))
+                for r in requests:                              # what came before: the same pages on every server, written on one
+                    p = s.plan([(r, context)])
+                    if s is servers[0]:
+                        s.iterate(before, p)
+                s.copy_cache(servers[0])
                 plans.append(s.plan([(r, 1) for r in requests[:n]] + [(r, chunk) for r in requests[n:]]))
             x = torch.randn((plans[0].tokens, block.width), generator=gen, device=device).to(block.dtype)
 

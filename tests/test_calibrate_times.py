@@ -40,3 +40,21 @@ def test_a_slow_host_is_not_in_the_times(monkeypatch):
     monkeypatch.setattr(I, "kv_write", slow)
     samples = K.measure(SMALL, [0], [1, 3], 20, passes=3, layers=2)
     assert all(0 < t < 0.001 for _, _, t in samples), samples
+
+
+@pytest.mark.gpu
+def test_caches_of_the_layers_hold_the_same_and_fit(monkeypatch):
+    servers = []
+    make = K.Server.__init__
+    monkeypatch.setattr(K.Server, "__init__", lambda self, *a, **kw: servers.append(self) or make(self, *a, **kw))
+    fp8 = K.Block(heads=4, kv_heads=2, head_dim=64, rank=8, classes=2, page=16)
+    K.measure(fp8, [0, 16], [0, 2], 50, passes=2, layers=3)
+    assert len(servers) == 3 and bool((servers[0].k.view(torch.uint8) != 0).any())
+    for s in servers[1:]:
+        # everything but the places of the last passes' tokens, which are not on all of the servers
+        same = [torch.equal(a.view(torch.uint8)[:, :, :2], b.view(torch.uint8)[:, :, :2]) for a, b in ((s.k, servers[0].k), (s.v, servers[0].v))]
+        assert all(same) and s.k.data_ptr() != servers[0].k.data_ptr()
+    servers.clear()
+    monkeypatch.setattr(torch.cuda, "mem_get_info", lambda *a: (0, 1 << 38))
+    K.measure(fp8, [0], [2], 20, passes=2, layers=3)
+    assert len(servers) == 1
