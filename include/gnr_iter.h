@@ -82,7 +82,7 @@ int iter_kv_read(const iter_cache *cache, int type, const iter_rows *k, const it
 /* A batch: request r brings the tokens q_start[r] .. q_start[r+1]-1 (one for a decode, a chunk for a prefill, none is
  * fine; a batch of tokens has a request), which are the last ones of the kv_len[r] that its cache holds; token j of a request lies at place j % page of
  * page page_table[r*table_stride + j / page]. All arrays on the device, q_start with requests + 1 entries ascending from 0 to `tokens`.
- * max_q is what the host expects of the longest chunk: it selects kernels, results do not depend on it being right. */
+ * max_q is what the host expects of the longest chunk: it selects kernels, results depend on it being right in nothing but their rounding. */
 typedef struct {
   int requests;
   int64_t tokens, max_q;
