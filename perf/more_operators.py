@@ -401,7 +401,9 @@ def run(state):
         return iteration.kv_read(s["k"], s["v"], s["slots"], s["k_exp"], s["v_exp"], dtype=s["dtype"])
     if s["op"] == "attention":
         return iteration.attention(s["q"], s["k"], s["v"], s["table"], s["q_start"], s["kv_len"], s["k_exp"], s["v_exp"], window=s["window"], max_q=max(s["q_lens"]))
-    iteration.copy_pages((s["k"], s["v"], s["k_exp"], s["v_exp"]), s["source"], s["target"], s["places"])
+    # a program has a cache for each layer
+    exps = ([None] * len(s["k"]),) * 2 if s["k_exp"] is None else (s["k_exp"], s["v_exp"])
+    iteration.copy_pages(list(zip(s["k"], s["v"], *exps)), s["source"], s["target"], s["places"])
     return _layers(s)
 
 
