@@ -87,7 +87,7 @@ class Weights:
 
 @dataclass
 class Plan:
-    """An iteration's batch on the device (`Server.plan`)."""
+    """An iteration's batch on the device (`Server.plan`). It is of no use once the pages of a request that it brings tokens of were moved."""
     q_start: torch.Tensor
     kv_len: torch.Tensor
     table: torch.Tensor
@@ -96,6 +96,8 @@ class Plan:
     tokens: int
     longest: int
     positions: Optional[torch.Tensor] = None
+    requests: Tuple[int, ...] = ()                              # that it brings tokens of
+    made: int = 0                                               # how often the server had changed requests' pages by then
 
 
 class Server:
@@ -110,6 +112,7 @@ class Server:
         self._held = [0] * pages                                # requests that a page belongs to
         self._pages, self._length, self._class = {}, {}, {}
         self._next = 0
+        self._changes, self._changed = 0, {}                    # times that requests' pages were changed under them, and the last of them for each request
 
     def bytes(self) -> int:
         """Of the cache."""
@@ -137,6 +140,7 @@ class Server:
             if self._held[page] == 0:
                 self._free.append(page)
         del self._length[r], self._class[r]
+        self._changed.pop(r, None)
 
     def _take(self, n: int) -> List[int]:
         taken = [self._free.pop() for _ in range(n)]
@@ -171,7 +175,8 @@ class Server:
 
     @torch.no_grad()
     def compact(self) -> int:
-        """Moves the pages in use together, to the lowest numbers; how many there are. Plans made before are of no use after it."""
+        """Moves the pages in use together, to the lowest numbers; how many there are. `iterate` refuses plans that were made before for a request whose pages were moved: what was planned is
+        iterated first."""
         used = sum(n > 0 for n in self._held)
         source = [p for p in range(used, len(self._held)) if self._held[p]]
         target = [p for p in range(used) if not self._held[p]]
@@ -180,9 +185,20 @@ class Server:
         new = dict(zip(source, target))
         for a, b in new.items():
             self._held[b], self._held[a] = self._held[a], 0
+        if new:
+            self._outdate([r for r, pages in self._pages.items() if any(p in new for p in pages)])
         self._pages = {r: [new.get(p, p) for p in pages] for r, pages in self._pages.items()}
         self._free = list(range(used, len(self._held)))[::-1]
         return used
+
+    def _outdate(self, requests: Sequence[int]) -> None:
+        """Plans that have been made for tokens of these requests are of no use any more."""
+        self._changes += 1
+        self._changed.update((r, self._changes) for r in requests)
+
+    def _outdated(self, p: Plan) -> bool:
+        # (a request that has left has no pages: as far as pages were moved or shared, others may have its)
+        return p.made < self._changes and any(r not in self._length or self._changed.get(r, 0) > p.made for r in p.requests)
 
     def _missing(self, r: int, n: int) -> int:
         """Pages that request r lacks for n tokens more."""
@@ -226,11 +242,14 @@ class Server:
         return Plan(self._whole(start, i32), self._whole([self._length[r] for r, _ in batch], i32),
                     self._whole([self._pages[r] + [0] * (width - len(self._pages[r])) for r, _ in batch], i32).view(len(batch), width),
                     self._whole(slots, torch.int64), self._whole([self._class[r] for r, _ in batch], i32), start[-1],
-                    max([n for _, n in batch] + [0]), self._whole(positions, torch.int64) if self.turns is not None else None)
+                    max([n for _, n in batch] + [0]), self._whole(positions, torch.int64) if self.turns is not None else None,
+                    tuple(r for r, n in batch if n), self._changes)
 
     @torch.no_grad()
     def iterate(self, x: torch.Tensor, p: Plan) -> torch.Tensor:
         """The block's output for the activations x [tokens, width] of a plan's tokens; their keys and values go to the cache."""
+        if self._outdated(p):
+            raise ValueError("the plan is of no use any more: pages of its requests were moved, or requests left, after it was made")
         b, w = self.block, self.weights
         qkv = x @ w.qkv.T
         iteration.adapters(x, qkv, *w.qkv_adapter, w.scale, p.q_start, p.adapter, out=qkv, status=self.status)
