@@ -87,7 +87,7 @@ class Weights:
 
 @dataclass
 class Plan:
-    """An iteration's batch on the device (`Server.plan`). It is of no use once the pages of a request that it brings tokens of were moved."""
+    """An iteration's batch on the device (`Server.plan`). It is of no use once a request that it brings tokens of went on in several ways or has its pages moved."""
     q_start: torch.Tensor
     kv_len: torch.Tensor
     table: torch.Tensor
@@ -154,7 +154,10 @@ class Server:
     @torch.no_grad()
     def fork(self, r: int, ways: int = 1) -> List[int]:
         """Requests that go on from what request r has, beside it: finished pages are shared, the last one, if it is not, is copied for each. They
-        are of r's class. MemoryError, and nothing changes, where there are not enough pages for the copies."""
+        are of r's class. MemoryError, and nothing changes, where there are not enough pages for the copies.
+
+        What r has are the tokens of the cache: those that were planned are iterated first. `iterate` refuses plans that were made before for r: copies would lack what they write, and shared
+        pages would change under the others."""
         if ways < 0:
             raise ValueError("a request cannot go on in fewer than no ways")
         page, n = self.block.page, self._length[r]
@@ -171,6 +174,8 @@ class Server:
                 self._held[shared] += 1
             self._pages[f], self._length[f] = full + self._take(1 if copies else 0), n
             forks.append(f)
+        if forks:
+            self._outdate([r])
         return forks
 
     @torch.no_grad()
@@ -249,7 +254,7 @@ class Server:
     def iterate(self, x: torch.Tensor, p: Plan) -> torch.Tensor:
         """The block's output for the activations x [tokens, width] of a plan's tokens; their keys and values go to the cache."""
         if self._outdated(p):
-            raise ValueError("the plan is of no use any more: pages of its requests were moved, or requests left, after it was made")
+            raise ValueError("the plan is of no use any more: requests of it went on in several ways, had their pages moved or left after it was made")
         b, w = self.block, self.weights
         qkv = x @ w.qkv.T
         iteration.adapters(x, qkv, *w.qkv_adapter, w.scale, p.q_start, p.adapter, out=qkv, status=self.status)

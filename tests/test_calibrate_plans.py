@@ -91,3 +91,47 @@ def test_plans_stay_where_no_page_of_theirs_moves(server):
     for r in (a, b, c):
         server.leave(r)
     assert not server._changed
+
+
+def test_a_plan_from_before_its_request_went_on_in_several_ways_is_refused(server):
+    r, other = server.admit(0), server.admit(0)
+    server.iterate(_tokens(1, 18), server.plan([(r, 18)]))
+    planned, apart = server.plan([(other, 1), (r, 2)]), server.plan([(other, 1)])
+    forks = server.fork(r, 2)
+    before = _state(server)
+    with pytest.raises(ValueError, match="several ways"):          # the forks' pages were copied without these tokens
+        server.iterate(_tokens(19, 3), planned)
+    assert _same(before, _state(server))
+    server.iterate(_tokens(70, 1), apart)                         # a plan of others
+    assert _reads(server, other)[1] == 70
+    server.leave(r)
+    with pytest.raises(ValueError, match="left"):
+        server.iterate(_tokens(19, 3), planned)
+    assert [_reads(server, f)[:18] for f in forks] == [list(range(1, 19))] * 2
+
+
+def test_a_plan_that_was_iterated_before_its_request_went_on(server):
+    r = server.admit(0)
+    p = server.plan([(r, 18)])
+    server.iterate(_tokens(1, 18), p)
+    assert server.fork(r, 0) == []
+    server.iterate(_tokens(1, 18), p)                             # there are no forks
+    (f,) = server.fork(r)
+    with pytest.raises(ValueError, match="several ways"):          # again: the first page is the fork's as well
+        server.iterate(_tokens(40, 18), p)
+    for first, q in ((60, r), (80, f)):
+        server.iterate(_tokens(first, 3), server.plan([(q, 3)]))
+    assert _reads(server, r) == list(range(1, 19)) + [60, 61, 62] and _reads(server, f) == list(range(1, 19)) + [80, 81, 82]
+    p = server.plan([(f, 2)])
+    (g,) = server.fork(r)                                         # r's, not f's
+    server.iterate(_tokens(83, 2), p)
+    assert _reads(server, f)[18:] == [80, 81, 82, 83, 84] and _reads(server, g) == _reads(server, r)
+
+
+def test_a_fork_without_room_leaves_plans_as_they_are(server):
+    r = server.admit(0)
+    p = server.plan([(r, 18)])
+    with pytest.raises(MemoryError):
+        server.fork(r, 11)
+    server.iterate(_tokens(1, 18), p)
+    assert _reads(server, r) == list(range(1, 19))
