@@ -107,7 +107,9 @@ class Server:
         self.block, self.weights, self.device = block, weights, torch.device(device)
         self.k, self.v, self.k_exp, self.v_exp = iteration.new_cache(pages, block.kv_heads, block.page, block.head_dim, block.cache, device)
         self.status = iteration.new_status(device)
-        self.turns = block.positions.turns(block.head_dim, device) if block.positions else None
+        turns = block.positions.turns(block.head_dim, "cpu") if block.positions else None
+        self.turns = turns.to(device) if turns is not None else None
+        self._turned = (turns.tolist(), block.positions.interleaved, block.positions.magnitude) if block.positions else None   # what its cached keys went through
         self._free = list(range(pages))[::-1]
         self._held = [0] * pages                                # requests that a page belongs to
         self._pages, self._length, self._class = {}, {}, {}
@@ -271,9 +273,11 @@ class Server:
 
     @torch.no_grad()
     def move(self, r: int, to: "Server") -> int:
-        """Moves a request with its cache to another server; its number there. If that one has no room for it, or a cache that is not
-        made for its rows, nothing changes on either."""
+        """Moves a request with its cache to another server; its number there. If that one has no room for it, a cache that is not
+        made for its rows or other positions (cached keys are turned already), nothing changes on either."""
         n = self._length[r]
+        if n and self._turned != to._turned:
+            raise ValueError("a request cannot move to a server whose block has other positions")
         to._need(-(-n // to.block.page))
         k, v = iteration.kv_read(self.k, self.v, self._whole(self._slots(r, range(n)), torch.int64), self.k_exp, self.v_exp, dtype=self.block.dtype)
         there = to.admit(self._class[r])

@@ -1,4 +1,6 @@
 """Plans of an iteration whose requests' pages change before it runs. The operators are stood in for: these are the host's books."""
+from dataclasses import replace
+
 import pytest
 import torch
 
@@ -135,3 +137,36 @@ def test_a_fork_without_room_leaves_plans_as_they_are(server):
         server.fork(r, 11)
     server.iterate(_tokens(1, 18), p)
     assert _reads(server, r) == list(range(1, 19))
+
+
+KINDS = [None, K.Positions(), K.Positions(base=500000.0), K.Positions(dims=32), K.Positions(interleaved=True), K.Positions(magnitude=1.1), K.Positions(scaling="linear", factor=2.0)]
+
+
+@pytest.mark.parametrize("mine", range(len(KINDS)))
+def test_a_request_stays_where_the_other_server_has_other_positions(mine, monkeypatch):
+    moved = []
+    monkeypatch.setattr(I, "kv_read", lambda k, v, slots, *a, **kw: (slots, slots))
+    monkeypatch.setattr(I, "kv_write", lambda *a: moved.append(a))
+    one, *others = (K.Server(replace(BLOCK, positions=p), None, 6, device="cpu") for p in [KINDS[mine]] + KINDS)
+    r, empty = one.admit(0), one.admit(0)
+    one.plan([(r, 20)])
+    for i, two in enumerate(others):
+        if i == mine:
+            continue
+        before = _state(one), _state(two), two._next
+        with pytest.raises(ValueError, match="positions"):
+            one.move(r, two)
+        assert _same(before[0], _state(one)) and _same(before[1], _state(two)) and two._next == before[2] and one.length(r) == 20 and not moved
+    assert others[(mine + 1) % len(others)].length(one.move(empty, others[(mine + 1) % len(others)])) == 0    # nothing was turned yet
+    moved.clear()
+    there = one.move(r, others[mine])
+    assert others[mine].length(there) == 20 and len(moved) == 1 and len(one._free) == 6
+
+
+def test_positions_that_are_written_in_other_words_are_the_same(monkeypatch):
+    monkeypatch.setattr(I, "kv_read", lambda k, v, slots, *a, **kw: (slots, slots))
+    monkeypatch.setattr(I, "kv_write", lambda *a: None)
+    one, two = (K.Server(replace(BLOCK, positions=p), None, 6, device="cpu") for p in (K.Positions(), K.Positions(dims=64, scaling="linear", factor=1.0)))
+    r = one.admit(0)
+    one.plan([(r, 20)])
+    assert two.length(one.move(r, two)) == 20
