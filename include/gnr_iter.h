@@ -143,7 +143,8 @@ typedef struct {
   const int64_t *turns;                                    /* device, dims / 2 */
 } iter_turns;
 
-/* Rows of `heads` heads of head_dim (64, 128 or 256) elements of `type` (BF16 or FP16), turned: out may be x itself (the same rows) or apart from it. */
+/* Rows of `heads` heads of head_dim (64, 128 or 256) elements of `type` (BF16 or FP16), turned: out may be x itself (the same rows) or apart from it: in other memory, beside it in
+ * the rows of one matrix, or with heads or tokens that alternate with x's at common strides. */
 int iter_rotary(int type, int heads, int head_dim, const iter_turns *turns, const int64_t *positions, int64_t tokens, const iter_rows *x,
                 const iter_rows *out, void *hip_stream);
 

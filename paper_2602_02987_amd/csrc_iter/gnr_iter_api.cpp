@@ -5,6 +5,7 @@
 #include <initializer_list>
 #include <memory>
 #include <new>
+#include <numeric>
 
 #include "gnr_iter_internal.h"
 
@@ -77,18 +78,42 @@ int check_batch(const iter_cache *c, const iter_batch *b, int heads)
   return SIM_OK;
 }
 
-// Whether rows of `heads` heads of `dim` elements share no element with others: their bytes lie apart, or they lie beside each other in the rows of one matrix, as a projection leaves
-// queries, keys and values.
+// The remainder of a division that is rounded down.
+int64_t remainder_of(int64_t n, int64_t d) { return (n % d + d) % d; }
+
+// Whether pieces of `dim` elements at `off` and any multiples of `step` from there leave those at 0 and any multiples of it alone.
+bool alternate(int64_t off, int64_t step, int dim)
+{
+  if (step < 2 * static_cast<int64_t>(dim)) return false;
+  const int64_t at = remainder_of(off, step);
+  return at >= dim && at + dim <= step;
+}
+
+// The stride of two counts of pieces, of which single ones have none; 0 if there is none in common.
+int64_t common(int64_t a, int64_t count_a, int64_t b, int64_t count_b) { return count_a > 1 && count_b > 1 ? (a == b ? a : 0) : count_a > 1 ? a : count_b > 1 ? b : 0; }
+
+// Whether pieces lie apart in the rows, `step` elements each, of one matrix, where those of a and b take `row_a` and `row_b`: beside each other, or, if neither's go on into the next row
+// of the other, in turn (`inner`: the greatest common divisor of the strides within a row).
+bool apart_in_matrix(int64_t between, int64_t step, int64_t row_a, int64_t row_b, int64_t inner, int dim)
+{
+  if (row_a > step || row_b > step) return false;
+  const int64_t beside = remainder_of(between, step);
+  if (beside >= row_a && beside + row_b <= step) return true;
+  return (beside + row_b <= step && alternate(beside, inner, dim)) || (step - beside + row_a <= step && alternate(beside - step, inner, dim));
+}
+
+// Whether rows of `heads` heads of `dim` elements share no element with others: their bytes lie apart, they alternate (two pieces are as far apart as the rows' beginnings and multiples of the
+// strides, which are multiples of the strides' greatest common divisor), or they lie apart in the rows of one matrix, as a projection leaves queries, keys and values, or in those of the heads.
 bool apart(const iter_rows &a, int heads_a, const iter_rows &b, int heads_b, int64_t tokens, int dim)
 {
   const uintptr_t at_a = reinterpret_cast<uintptr_t>(a.data), at_b = reinterpret_cast<uintptr_t>(b.data);
-  const int64_t row_a = (heads_a - 1) * a.head_stride + dim, row_b = (heads_b - 1) * b.head_stride + dim;
-  const uintptr_t end_a = at_a + 2 * static_cast<uintptr_t>((tokens - 1) * a.token_stride + row_a), end_b = at_b + 2 * static_cast<uintptr_t>((tokens - 1) * b.token_stride + row_b);
+  const int64_t token_a = (heads_a - 1) * a.head_stride + dim, token_b = (heads_b - 1) * b.head_stride + dim, head_a = (tokens - 1) * a.token_stride + dim, head_b = (tokens - 1) * b.token_stride + dim;
+  const uintptr_t end_a = at_a + 2 * static_cast<uintptr_t>(head_a - dim + token_a), end_b = at_b + 2 * static_cast<uintptr_t>(head_b - dim + token_b);
   if (end_a <= at_b || end_b <= at_a) return true;
-  const int64_t step = a.token_stride;
-  if (tokens == 1 || step != b.token_stride || row_a > step || row_b > step) return false;
-  const int64_t off = static_cast<int64_t>(at_b - at_a) / 2 % step, beside = off < 0 ? off + step : off;
-  return beside >= row_a && beside + row_b <= step;
+  const int64_t between = static_cast<int64_t>(at_b - at_a) / 2;
+  const int64_t heads = std::gcd(heads_a > 1 ? a.head_stride : 0, heads_b > 1 ? b.head_stride : 0), all = tokens > 1 ? std::gcd(a.token_stride, b.token_stride) : 0;
+  return alternate(between, std::gcd(heads, all), dim) || apart_in_matrix(between, common(a.token_stride, tokens, b.token_stride, tokens), token_a, token_b, heads, dim) ||
+         apart_in_matrix(between, common(a.head_stride, heads_a, b.head_stride, heads_b), head_a, head_b, all, dim);
 }
 
 bool same_rows(const iter_rows &a, const iter_rows &b, int64_t tokens, int heads)
