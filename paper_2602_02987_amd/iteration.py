@@ -168,12 +168,14 @@ def adapters(x, base, down, up, scale, q_start, adapter, out=None, workspace=Non
 def rotary_frequencies(dims, base=10000.0, scaling=None, factor=1.0, original=8192, low=1.0, high=4.0):
     """Radians a position of dims / 2 pairs, base ** (-2 i / dims), scaled for contexts `factor` times as long as the `original` one:
 
-    None: as they are. "linear": all divided by the factor. "base": the base raised by factor ** (dims / (dims - 2)), which divides the slowest by the factor and leaves the fastest. "parts": those that make
+    None: as they are (the factor has to be 1). "linear": all divided by the factor. "base": the base raised by factor ** (dims / (dims - 2)), which divides the slowest by the factor and leaves the fastest. "parts": those that make
     at least `high` turns in the original context stay, those with at most `low` are divided by the factor, and between them the two are mixed in proportion to the turns."""
     if dims < 2 or dims % 2 or base <= 0 or factor <= 0 or original <= 0:
         raise ValueError("dims has to be even, base, factor and original positive")
     if scaling not in (None, "linear", "base", "parts"):
         raise ValueError("scaling has to be None, 'linear', 'base' or 'parts'")
+    if scaling is None and factor != 1.0:
+        raise ValueError("a factor needs a scaling that uses it")
     if scaling == "base":
         if dims == 2:
             raise ValueError("a single pair has no slowest and fastest frequency")
