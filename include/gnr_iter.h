@@ -48,7 +48,7 @@ enum iter_status { ITER_BAD_BATCH = 1, ITER_BAD_PAGE = 2, ITER_BAD_ADAPTER = 4 }
  * place*place_stride + d], strides in elements, non-negative (place_stride and exp_place_stride at most 2^24), the data and every row 16-byte aligned. Of an FP8 cache the row (page, head,
  * place) stands for its codes times 2^(exp - 127), where exp is the byte at exp[page*exp_page_stride + head*exp_head_stride +
  * place*exp_place_stride] (1..254). Of an FP4 cache every 32 elements of a row have a byte of their own, which follow each other: that of the elements from 32*i on is i
- * bytes further on, and one of 255 stands for 32 that are no numbers; strides count elements, two of which are a byte. Other caches have no exponents (NULL). */
+ * bytes further on (1..254; what a byte of 0 reads as is not said), and one of 255 stands for 32 that are no numbers; strides count elements, two of which are a byte. Other caches have no exponents (NULL). */
 typedef struct {
   void *data;                                              /* device */
   uint8_t *exp;                                            /* device */

@@ -16,7 +16,8 @@ constexpr int kPartTail = 4;                   // words of a part after its sums
 // of kKeys keys.
 struct RowsShape { static constexpr int kRows = 16, kKeys = 32 * kWaves, kPlan = 0; };
 struct ChunkShape { static constexpr int kRows = 128, kKeys = 64, kPlan = 1; };
-// Workgroups that a compute unit holds at once, by their registers. Few rows of 256 elements over 4 bits fit twice, over 8 and 16 bits
+// Workgroups that a compute unit holds at once, by their registers. Shared memory (34.6 KB of a workgroup with 128 elements, 67.4 with 256, and 20 bytes a request) holds as many too, but over 4 bits
+// only up to 999 requests with 128 elements and 726 with 256: of more, the last third or half of the workgroups begin when others end, with the same results. Few rows of 256 elements over 4 bits fit twice, over 8 and 16 bits
 // once: 60 ragged decodes around 2000 keys (16 heads over 4) 74 -> 57 us with the second, 127 of them 137 -> 122, 3 around 30000
 // 43 -> 39, one of 1093 keys 16.6 -> 16.4. A fourth at 64 elements would spill (127 ragged decodes 160 -> 144 us, but 3 around 60000
 // keys 20 -> 26).
@@ -105,7 +106,7 @@ __device__ __forceinline__ int tiles_of(const AttentionParams &p, const Request 
 //
 // Few rows: all blocks of keys of all (tile, kv head) in a row, cut into as many pieces of the same length as there are workgroups: every one reads as
 // much of the cache, however long the requests are. Over 4 bits, where a block takes 3 us and the change from one tile to the next three times as long, a tile counts for three blocks more than it has: a workgroup with many short ones
-// was the last by far (127 decodes of 435000 keys in all, ragged: 127 -> 112 us; of 100 with 500 on the average 46 -> 34; counted for two blocks 114 and 34, for six 116 and 36). A (tile, kv head) that is cut leaves parts, two at most to a workgroup: one that began
+// was the last by far (127 decodes of 453000 keys in all, ragged: 127 -> 112 us; of 100 with 500 on the average 46 -> 34; counted for two blocks 114 and 34, for six 116 and 36). A (tile, kv head) that is cut leaves parts, two at most to a workgroup: one that began
 // before it (slot 0) and one that ends after it or is cut at its very beginning (slot 1).
 struct RowsPlan {
   int64_t *start;           // blocks of keys before request r, for one kv head

@@ -11,8 +11,8 @@ namespace gnr {
 // fourth block of 32 keys with a running maximum and sum of its own; the waves are joined at the end.
 //   Bound by the memory: sixteen rows of products for a key are far below the matrix rate. 127 decodes of 435000 keys beside a chunk (1.8 GB, 16 bits): 374 us in all,
 // 4.8 TB/s; 32 decodes of 100000 keys in 8 bits: 46 us, 4.5 TB/s. A single decode of 1093 keys takes 8 us: the chain from bounds to page table to keys to values.
-//   In 4 bits codes go through the conversion instructions as well: the scaled matrix instructions would take them as they are, but add their products with too few bits (with operands of a wide
-// range errors of 2^-14 of the sum of their magnitudes were seen). 127 decodes of 435000 keys (0.47 GB): 106 us, 4.5 TB/s, vector instructions 53 % of the cycles. A workgroup has 2.3 tiles of
+//   In 4 bits codes go through the conversion instructions as well: the scaled matrix instructions would take them as they are, but the queries and weights would have to be codes of 8 bits or fewer
+// there too. 127 decodes of 453000 keys (0.49 GB): 106 to 109 us, 4.5 to 4.7 TB/s, vector instructions 53 % of the cycles. A workgroup has 2.3 tiles of
 // these on the average, and between two of them nothing on its way. Three workgroups a compute unit instead of two: 132 -> 125 us with the join (before tiles counted for more than their keys, see RowsPlan); two blocks of keys on
 // their way at once change nothing.
 // Three decodes of 131000 keys (0.21 GB): 49 us, 4.4 TB/s.
